@@ -39,6 +39,12 @@
  *     nothing is launched and no output is touched.  No exception or abort
  *     crosses this interface.
  *   - Calls that share a workspace or an output and overlap in time race.
+ *
+ * Beside the convolution's operations stand those of a block with several
+ * experts (a layer in which every group of rows has a filter of its own), at
+ * the end of this header: the products grouped by expert with their two
+ * gradients, the norms around a block with its gate and residual scale, and
+ * the norm and clipping of all gradients.  They keep the same conventions.
  */
 #ifndef CONVBWD_H
 #define CONVBWD_H
@@ -343,6 +349,156 @@ int cbw_read_occupancy(const cbw_conv_desc* desc, const void* workspace, size_t 
  * CBW_OP_BWD_DATA (covers both data-gradient entry points),
  * CBW_OP_BWD_WEIGHT or CBW_OP_FWD; NULL events switch the hook off. */
 int cbw_set_profile_events(int op, void* start, void* stop);
+
+/* ------------------------------------------------ products grouped by expert
+ *
+ * A 1x1 convolution in which every group of rows has a filter of its own: row
+ * r of expert e, offsets[e] <= r < offsets[e + 1], meets W[e], stored [K][C]
+ * with the input features innermost (KRSC).
+ *
+ *   Y[r,k]    = sum_c X[r,c] W[e,k,c]                (ReLU with CBW_FLAG_RELU)
+ *   dX[r,c]   = live[r,c] ? sum_k dY[r,k] W[e,k,c] : +0.0
+ *   dW[e,k,c] = sum_{r of e} dY[r,k] X[r,c]          (float32; 0 without rows)
+ *
+ * offsets: E + 1 non-decreasing int32 in DEVICE memory (a router's counts,
+ * summed up), so no length passes through the host: any expert may have no
+ * row, one, or all.  Rows before offsets[0] and from offsets[E] on belong to
+ * no expert: they are neither read nor written.  Offsets outside [0, rows]
+ * are clamped to it; decreasing ones leave the result undefined, but no
+ * offsets make a call read or write outside its tensors. */
+typedef struct {
+    int32_t E;               /* experts, at most CBW_MAX_EXPERTS               */
+    int32_t C, K;            /* input and output features of a filter          */
+    int32_t dtype;           /* cbw_dtype of X, W, Y and of dX, dY             */
+    int64_t rows;            /* rows of X and Y (a capacity); 0 is allowed     */
+    int64_t x_stride;        /* elements from a row of X (dX) to the next      */
+    int64_t y_stride;        /* the same of Y (dY)                             */
+} cbw_expert_desc;
+#define CBW_MAX_EXPERTS 1024
+
+/* expert_fwd: Y = relu of the product; without it the product itself. */
+#define CBW_FLAG_RELU 4u
+
+/* Host-only check.  CBW_ERR_UNSUPPORTED: C or K (or a stride) not a multiple of
+ * the 16-byte vector (8 bf16, 4 float32), a filter of 2^31 bytes or more (its
+ * float32 gradient counts), more than 2^31 - 1 rows, more than CBW_MAX_EXPERTS
+ * experts, a stride of 2^20 elements or more. */
+int cbw_validate_expert_desc(const cbw_expert_desc* desc);
+
+/* Workspace bytes, enough for each of the three calls (host only). */
+int cbw_expert_workspace_size(const cbw_expert_desc* desc, size_t* bytes);
+
+/* Y from X[rows][C] and W[E][K][C].  y_mask (nullable): the footprint bits
+ * (Y > 0) of the experts' rows, bit r*K + k (as cbw_relu_mask_pack on a
+ * contiguous Y), ceil(rows*K/32) words, 4-byte aligned; K a multiple of 32 and CBW_FLAG_RELU are
+ * needed for it.  float32 accumulation, one rounding to bf16. */
+int expert_fwd(const cbw_expert_desc* desc, const void* X, const void* W, const int32_t* offsets, void* Y,
+               uint32_t* y_mask, void* workspace, size_t workspace_bytes, uint32_t flags, void* stream);
+
+/* dX from dY[rows][K] and W.  x_mask (nullable, 4-byte aligned): footprint of
+ * X, bit r*C + c of ceil(rows*C/32) words; dead values are written as +0.0. */
+int expert_bwd_data(const cbw_expert_desc* desc, const void* dY, const void* W, const int32_t* offsets,
+                    const uint32_t* x_mask, void* dX, void* workspace, size_t workspace_bytes, void* stream);
+
+/* dW[E][K][C] (float32, fully overwritten) from X and dY.  Deterministic: the
+ * rows' partial sums are added in a fixed order. */
+int expert_bwd_weight(const cbw_expert_desc* desc, const void* X, const void* dY, const int32_t* offsets, float* dW,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------- norms around a block, gate, residual scale
+ *
+ * x is the residual stream, u the block's output, g its gate, s the scale of
+ * the residual branch; y the stream after the block, h the next block's input:
+ *
+ *   y = x + s act(g) N_post(u),   h = N_pre(y)
+ *   N(v) = (v - mu) r w + b,  r = 1 / sqrt(mean((v - mu)^2) + eps)
+ *
+ * over the C values of a row (of NHWC tensors: a pixel), mu = 0 for
+ * CBW_NORM_RMS.  Statistics are float32; y and h are rounded once, h from the
+ * unrounded y.  One gate row serves gate_rows consecutive rows (1: each row
+ * has its own; a pixel count: one gate per image and channel); gate has
+ * ceil(rows / gate_rows) rows. */
+enum { CBW_NORM_NONE = 0, CBW_NORM_RMS = 1, CBW_NORM_LAYER = 2 };
+enum { CBW_GATE_NONE = 0, CBW_GATE_LINEAR = 1, CBW_GATE_SIGMOID = 2 };
+typedef struct {
+    int64_t rows;                       /* 0 is allowed                          */
+    int64_t gate_rows;                  /* rows per gate row, at least 1         */
+    int64_t res_stride;                 /* elements between rows: x, y, dx, dy   */
+    int64_t block_stride;               /* u, h, du, dh                          */
+    int64_t gate_stride;                /* gate, dgate                           */
+    int32_t C;
+    int32_t dtype;                      /* cbw_dtype of u, h, gate, their gradients */
+    int32_t res_dtype;                  /* of x, y, dx, dy; float32 where dtype is */
+    int32_t pre_norm, post_norm;        /* CBW_NORM_*; either may be NONE        */
+    int32_t gate_act;                   /* CBW_GATE_*                            */
+    float eps;                          /* finite, not negative                  */
+} cbw_norm_desc;
+
+/* The norms' weights and biases and the scale: float32, C values each, 16-byte
+ * aligned; NULL: weight 1, bias 0, scale 1.  Those of a norm that the
+ * descriptor leaves out are NULL.  Also the gradients of block_norm_bwd, where
+ * NULL asks for none. */
+typedef struct {
+    float *w_pre, *b_pre, *w_post, *b_post, *scale;
+} cbw_norm_params;
+
+/* Host-only check.  CBW_ERR_UNSUPPORTED: C over 16384, C or a stride not a
+ * multiple of 8, a bf16 stream beside a float32 block. */
+int cbw_validate_norm_desc(const cbw_norm_desc* desc);
+
+/* Workspace bytes of block_norm_bwd (host only). */
+int cbw_norm_workspace_size(const cbw_norm_desc* desc, size_t* bytes);
+
+/* u NULL: there is no block before (the first one's input norm): h = N_pre(x),
+ * gate and y NULL.  h NULL where pre_norm is CBW_NORM_NONE, and only there.
+ * gate NULL where gate_act is CBW_GATE_NONE, and only there (or where u is).
+ * stats (nullable): float32 [rows][4], mu and r of y, mu and r of u (0 where
+ * there is none), which the backward pass reads; 16-byte aligned.  y may be x. */
+int block_norm_fwd(const cbw_norm_desc* desc, const void* x, const void* u, const void* gate,
+                   const cbw_norm_params* params, void* y, void* h, float* stats, void* stream);
+
+/* The gradients from those of y (dy, nullable: none comes) and of h (dh; NULL
+ * where pre_norm is NONE, and only there): dx (also the one of the stream that
+ * enters the block), du, dgate (nullable), and the parameters'.  y, u, gate,
+ * params and stats as block_norm_fwd had or gave them; without a block (u
+ * NULL) y is its x and gate, du and dgate are NULL.  Parameter gradients are
+ * overwritten; the sums over rows have a fixed order.  With rows = 0 they are
+ * zero.  dx may be dy.  */
+int block_norm_bwd(const cbw_norm_desc* desc, const void* y, const void* u, const void* gate,
+                   const cbw_norm_params* params, const float* stats, const void* dy, const void* dh, void* dx,
+                   void* du, void* dgate, const cbw_norm_params* grads, void* workspace, size_t workspace_bytes,
+                   void* stream);
+
+/* --------------------------------------- norm and clipping of all gradients
+ *
+ * grads is a HOST array of n entries, read during the call only; the tensors
+ * are in device memory, of any alignment that suits their type, and may be
+ * empty.  The 2-norm is summed in 64 bits in a fixed order. */
+typedef struct {
+    const void* grad;
+    void* out;               /* grad_clip: where the scaled values go; may be grad */
+    int64_t count;           /* elements                                           */
+    int32_t dtype;           /* cbw_dtype of grad and out                          */
+    int32_t reserved;        /* 0                                                  */
+} cbw_grad;
+enum { CBW_GRAD_NORM_2 = 0, CBW_GRAD_NORM_INF = 1 };
+
+/* Workspace bytes of the two calls (host only). */
+int cbw_grad_workspace_size(const cbw_grad* grads, int32_t n, size_t* bytes);
+
+/* norm[0] (device float32) = the norm of all tensors taken together, 0 for
+ * none; NaN if any value is, infinity if any is (the 2-norm of finite values
+ * that exceeds float32's range as well). */
+int grad_norm(const cbw_grad* grads, int32_t n, int32_t kind, float* norm, void* workspace, size_t workspace_bytes,
+              void* stream);
+
+/* out = grad * c with c = min(1, max_norm / (norm + 1e-6)); norm (device
+ * float32[2]) receives the norm and c.  Nothing is read back: a norm that is
+ * infinite gives c = 0 and one that is NaN c = NaN, and the caller who wants
+ * to leave out such a step tests norm[0].  A tensor in place (out == grad) is
+ * not touched when c is 1.  max_norm is not negative. */
+int grad_clip(const cbw_grad* grads, int32_t n, int32_t kind, float max_norm, float* norm, void* workspace,
+              size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

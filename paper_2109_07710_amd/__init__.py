@@ -26,13 +26,23 @@ CBW_OP_BWD_DATA, CBW_OP_BWD_DATA_MASKED, CBW_OP_BWD_WEIGHT, CBW_OP_FWD, CBW_OP_B
 CBW_OP_BWD_BOTH = 5
 CBW_FLAG_NO_SKIP = 1
 CBW_FLAG_SKIP_X_BLOCKS = 2
+CBW_FLAG_RELU = 4
+CBW_MAX_EXPERTS = 1024
+CBW_NORM_NONE, CBW_NORM_RMS, CBW_NORM_LAYER = 0, 1, 2
+CBW_GATE_NONE, CBW_GATE_LINEAR, CBW_GATE_SIGMOID = 0, 1, 2
+CBW_GRAD_NORM_2, CBW_GRAD_NORM_INF = 0, 1
 
 EXPORTS = ("cbw_status_string", "cbw_validate_desc", "cbw_mask_words", "cbw_dy_mask_words",
            "cbw_workspace_size", "cbw_data_tiling", "cbw_relu_mask_pack", "cbw_nonzero_mask_pack", "conv_bwd_data",
            "conv_bwd_data_masked", "conv_bwd_data_masked_noalloc", "conv_fwd_relu_mask", "conv_bwd_weight_sparse", "conv_bwd_weight_sparse_x", "conv_bwd_sparse",
            "conv_bwd_data_elementwise", "cbw_read_pixel_counts", "cbw_read_weight_work", "cbw_read_stats",
            "cbw_read_live_lists",
-           "cbw_read_occupancy", "cbw_set_profile_events")
+           "cbw_read_occupancy", "cbw_set_profile_events",
+           "cbw_validate_expert_desc", "cbw_expert_workspace_size", "expert_fwd", "expert_bwd_data", "expert_bwd_weight",
+           "cbw_validate_norm_desc", "cbw_norm_workspace_size", "block_norm_fwd", "block_norm_bwd",
+           "cbw_grad_workspace_size", "grad_norm", "grad_clip")
+
+_DTYPES = {"bf16": CBW_BF16, "f32": CBW_F32}
 
 
 class ConvDesc(ctypes.Structure):
@@ -58,6 +68,66 @@ class ConvDesc(ctypes.Structure):
 class Stats(ctypes.Structure):
     _fields_ = [("rows_total", ctypes.c_int64), ("rows_live", ctypes.c_int64),
                 ("blocks_total", ctypes.c_int64), ("blocks_skipped", ctypes.c_int64)]
+
+
+class ExpertDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("E", "C", "K", "dtype")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "x_stride", "y_stride")]
+
+    @classmethod
+    def make(cls, E, rows, C, K, dtype="bf16", x_stride=None, y_stride=None):
+        return cls(E, C, K, _DTYPES[dtype], rows, C if x_stride is None else x_stride,
+                   K if y_stride is None else y_stride)
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "gate_rows", "res_stride", "block_stride", "gate_stride")] + \
+               [(n, ctypes.c_int32) for n in ("C", "dtype", "res_dtype", "pre_norm", "post_norm", "gate_act")] + \
+               [("eps", ctypes.c_float)]
+
+    @classmethod
+    def make(cls, rows, C, pre="rms", post="rms", gate="none", gate_rows=1, dtype="bf16", res_dtype="bf16", eps=1e-5,
+             res_stride=None, block_stride=None, gate_stride=None):
+        kinds = {"none": CBW_NORM_NONE, "rms": CBW_NORM_RMS, "layer": CBW_NORM_LAYER}
+        acts = {"none": CBW_GATE_NONE, "linear": CBW_GATE_LINEAR, "sigmoid": CBW_GATE_SIGMOID}
+        return cls(rows, gate_rows, *(C if s is None else s for s in (res_stride, block_stride, gate_stride)), C,
+                   _DTYPES[dtype], _DTYPES[res_dtype], kinds[pre], kinds[post], acts[gate], eps)
+
+
+class NormParams(ctypes.Structure):
+    """Weights and biases of a block's norms and its residual scale (or their
+    gradients): float32 device tensors of C values, or None.  Keeps the tensors."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("_w_pre", "_b_pre", "_w_post", "_b_post", "_scale")]
+
+    def __init__(self, w_pre=None, b_pre=None, w_post=None, b_post=None, scale=None):
+        self.tensors = (w_pre, b_pre, w_post, b_post, scale)
+        super().__init__(*(None if t is None else _typed(t, CBW_F32).data_ptr() for t in self.tensors))
+
+
+class _Grad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class GradList:
+    """The gradients of a model for grad_norm and grad_clip, and where their
+    scaled values go (in place without `outs`).  Keeps the tensors: a program
+    makes the list once and uses it as long as its gradients stay where they are."""
+
+    def __init__(self, grads, outs=None):
+        self.grads = list(grads)
+        self.outs = self.grads if outs is None else list(outs)
+        if len(self.outs) != len(self.grads):
+            raise ValueError("as many outputs as gradients")
+        self.array = (_Grad * max(len(self.grads), 1))()
+        for i, (g, o) in enumerate(zip(self.grads, self.outs)):
+            dt = _dtype_of(g)
+            if o.numel() != g.numel():
+                raise ValueError("an output has the size of its gradient")
+            self.array[i] = _Grad(_typed(g, dt).data_ptr(), _typed(o, dt).data_ptr(), g.numel(), dt, 0)
+
+    def __len__(self):
+        return len(self.grads)
 
 
 class CbwError(RuntimeError):
@@ -106,6 +176,20 @@ def lib():
     L.cbw_read_live_lists.argtypes = [dp, vp, sz, ctypes.c_int, vp, i32p, i32p, vp]
     L.cbw_read_occupancy.argtypes = [dp, vp, sz, vp, i32p, i32p, i32p, i32p, vp]
     L.cbw_set_profile_events.argtypes = [ctypes.c_int, vp, vp]
+    ep, np_, pp, gp = (ctypes.POINTER(t) for t in (ExpertDesc, NormDesc, NormParams, _Grad))
+    u32, i32 = ctypes.c_uint32, ctypes.c_int32
+    L.cbw_validate_expert_desc.argtypes = [ep]
+    L.cbw_expert_workspace_size.argtypes = [ep, ctypes.POINTER(sz)]
+    L.expert_fwd.argtypes = [ep, vp, vp, vp, vp, vp, vp, sz, u32, vp]
+    L.expert_bwd_data.argtypes = [ep, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.expert_bwd_weight.argtypes = [ep, vp, vp, vp, vp, vp, sz, vp]
+    L.cbw_validate_norm_desc.argtypes = [np_]
+    L.cbw_norm_workspace_size.argtypes = [np_, ctypes.POINTER(sz)]
+    L.block_norm_fwd.argtypes = [np_, vp, vp, vp, pp, vp, vp, vp, vp]
+    L.block_norm_bwd.argtypes = [np_, vp, vp, vp, pp, vp, vp, vp, vp, vp, vp, pp, vp, sz, vp]
+    L.cbw_grad_workspace_size.argtypes = [gp, i32, ctypes.POINTER(sz)]
+    L.grad_norm.argtypes = [gp, i32, i32, vp, vp, sz, vp]
+    L.grad_clip.argtypes = [gp, i32, i32, ctypes.c_float, vp, vp, sz, vp]
     for name in EXPORTS:
         if name != "cbw_status_string" and name not in ("cbw_mask_words", "cbw_dy_mask_words"):
             getattr(L, name).restype = ctypes.c_int
@@ -131,6 +215,55 @@ def _ptr(t):
     if not t.is_contiguous():
         raise ValueError("expected a contiguous tensor")
     return ctypes.c_void_p(t.data_ptr())
+
+
+def _dtype_of(t):
+    """The library's type of a tensor."""
+    import torch
+    if t.dtype == torch.bfloat16:
+        return CBW_BF16
+    if t.dtype == torch.float32:
+        return CBW_F32
+    raise ValueError("expected a bfloat16 or float32 tensor, got %s" % t.dtype)
+
+
+def _typed(t, dtype):
+    """A contiguous device tensor of the library's type `dtype`, as it is."""
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    if not t.is_contiguous():
+        raise ValueError("expected a contiguous tensor")
+    if _dtype_of(t) != dtype:
+        raise ValueError("expected a %s tensor" % ("float32" if dtype == CBW_F32 else "bfloat16"))
+    return t
+
+
+def _rows(t, rows, cols, stride, dtype):
+    """Device pointer of a row tensor [rows][cols] of the given type whose
+    rows lie `stride` elements apart (None -> NULL)."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError("expected a tensor of shape (%d, %d), got %s" % (rows, cols, tuple(t.shape)))
+    if rows > 0 and (t.stride(1) != 1 and cols > 1 or t.stride(0) != stride and rows > 1):
+        raise ValueError("expected rows %d elements apart, got strides %s" % (stride, t.stride()))
+    if _dtype_of(t) != dtype:
+        raise ValueError("expected a %s tensor" % ("float32" if dtype == CBW_F32 else "bfloat16"))
+    return t.data_ptr()
+
+
+def _whole(t, numel, torch_dtype):
+    """Device pointer of a contiguous tensor of at least `numel` elements of
+    the given torch type (None -> NULL)."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    if t.dtype != torch_dtype or t.numel() < numel or not t.is_contiguous():
+        raise ValueError("expected a contiguous %s tensor of %d elements" % (torch_dtype, numel))
+    return t.data_ptr()
 
 
 def _stream(stream):
@@ -311,3 +444,156 @@ def cbw_set_profile_events(op, start=None, stop=None):
         return ctypes.c_void_p(e if isinstance(e, int) else e.cuda_event)
     sp, tp = handle(start), handle(stop)
     _check(lib().cbw_set_profile_events(op, sp, tp), "cbw_set_profile_events")
+
+
+# ------------------------------------------------- products grouped by expert
+
+def _bytes(call, arg, *more):
+    n = ctypes.c_size_t(0)
+    _check(getattr(lib(), call)(arg, *more, ctypes.byref(n)), call)
+    return n.value
+
+
+def _workspace_of(nbytes, device):
+    import torch
+    return torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
+
+
+def cbw_validate_expert_desc(desc):
+    return lib().cbw_validate_expert_desc(ctypes.byref(desc))
+
+
+def cbw_expert_workspace_size(desc):
+    return _bytes("cbw_expert_workspace_size", ctypes.byref(desc))
+
+
+def expert_workspace(desc, device="cuda"):
+    """A uint8 device tensor of the size the three expert calls need."""
+    return _workspace_of(cbw_expert_workspace_size(desc), device)
+
+
+def _filters(d, W):
+    import torch
+    if tuple(W.shape) != (d.E, d.K, d.C):
+        raise ValueError("expected filters of shape (%d, %d, %d), got %s" % (d.E, d.K, d.C, tuple(W.shape)))
+    return _whole(W, d.E * d.K * d.C, torch.float32 if d.dtype == CBW_F32 else torch.bfloat16)
+
+
+def _offsets(d, offsets):
+    import torch
+    return _whole(offsets, d.E + 1, torch.int32)
+
+
+def expert_fwd(desc, X, W, offsets, Y, y_mask, ws, flags=0, stream=None):
+    """Y = X W[e]^T for the rows of every expert e, [offsets[e], offsets[e+1])
+    (offsets: int32 on the device); CBW_FLAG_RELU: its ReLU, and y_mask its
+    footprint bits (int32 words, or None)."""
+    import torch
+    d = desc
+    _check(lib().expert_fwd(ctypes.byref(d), _rows(X, d.rows, d.C, d.x_stride, d.dtype), _filters(d, W),
+                            _offsets(d, offsets), _rows(Y, d.rows, d.K, d.y_stride, d.dtype),
+                            _whole(y_mask, (d.rows * d.K + 31) // 32, torch.int32), _ptr(ws), _nbytes(ws), flags,
+                            _stream(stream)), "expert_fwd")
+
+
+def expert_bwd_data(desc, dY, W, offsets, x_mask, dX, ws, stream=None):
+    """dX = dY W[e], +0.0 where x_mask (None: everywhere live) is dead."""
+    import torch
+    d = desc
+    _check(lib().expert_bwd_data(ctypes.byref(d), _rows(dY, d.rows, d.K, d.y_stride, d.dtype), _filters(d, W),
+                                 _offsets(d, offsets), _whole(x_mask, (d.rows * d.C + 31) // 32, torch.int32),
+                                 _rows(dX, d.rows, d.C, d.x_stride, d.dtype), _ptr(ws), _nbytes(ws), _stream(stream)),
+           "expert_bwd_data")
+
+
+def expert_bwd_weight(desc, X, dY, offsets, dW, ws, stream=None):
+    """dW[e] = dY^T X over the rows of every expert e, float32 [E][K][C]."""
+    import torch
+    d = desc
+    if tuple(dW.shape) != (d.E, d.K, d.C):
+        raise ValueError("expected gradients of shape (%d, %d, %d), got %s" % (d.E, d.K, d.C, tuple(dW.shape)))
+    _check(lib().expert_bwd_weight(ctypes.byref(d), _rows(X, d.rows, d.C, d.x_stride, d.dtype),
+                                   _rows(dY, d.rows, d.K, d.y_stride, d.dtype), _offsets(d, offsets),
+                                   _whole(dW, d.E * d.K * d.C, torch.float32), _ptr(ws), _nbytes(ws), _stream(stream)),
+           "expert_bwd_weight")
+
+
+# -------------------------------- norms around a block, gate, residual scale
+
+def cbw_validate_norm_desc(desc):
+    return lib().cbw_validate_norm_desc(ctypes.byref(desc))
+
+
+def cbw_norm_workspace_size(desc):
+    return _bytes("cbw_norm_workspace_size", ctypes.byref(desc))
+
+
+def norm_workspace(desc, device="cuda"):
+    """A uint8 device tensor of the size block_norm_bwd needs."""
+    return _workspace_of(cbw_norm_workspace_size(desc), device)
+
+
+def _params(p, C):
+    if p is None:
+        return None
+    for t in p.tensors:
+        if t is not None and t.numel() != C:
+            raise ValueError("expected parameters of %d values, got %d" % (C, t.numel()))
+    return ctypes.byref(p)
+
+
+def _gate(d, gate):
+    return _rows(gate, (d.rows + d.gate_rows - 1) // d.gate_rows, d.C, d.gate_stride, d.dtype)
+
+
+def block_norm_fwd(desc, x, u, gate, params, y, h, stats=None, stream=None):
+    """y = x + scale * act(gate) * N_post(u), h = N_pre(y); u, gate and y None:
+    h = N_pre(x).  stats (float32 [rows][4], or None): what the backward needs."""
+    import torch
+    d = desc
+    res = lambda t: _rows(t, d.rows, d.C, d.res_stride, d.res_dtype)  # noqa: E731
+    blk = lambda t: _rows(t, d.rows, d.C, d.block_stride, d.dtype)  # noqa: E731
+    _check(lib().block_norm_fwd(ctypes.byref(d), res(x), blk(u), _gate(d, gate), _params(params, d.C), res(y), blk(h),
+                                _whole(stats, 4 * d.rows, torch.float32), _stream(stream)), "block_norm_fwd")
+
+
+def block_norm_bwd(desc, y, u, gate, params, stats, dy, dh, dx, du, dgate, grads, ws, stream=None):
+    """The gradients of block_norm_fwd's inputs from dy and dh; dy, du, dgate
+    and each of grads (a NormParams) may be None."""
+    import torch
+    d = desc
+    res = lambda t: _rows(t, d.rows, d.C, d.res_stride, d.res_dtype)  # noqa: E731
+    blk = lambda t: _rows(t, d.rows, d.C, d.block_stride, d.dtype)  # noqa: E731
+    _check(lib().block_norm_bwd(ctypes.byref(d), res(y), blk(u), _gate(d, gate), _params(params, d.C),
+                                _whole(stats, 4 * d.rows, torch.float32), res(dy), blk(dh), res(dx), blk(du),
+                                _gate(d, dgate), _params(grads, d.C), _ptr(ws), _nbytes(ws), _stream(stream)),
+           "block_norm_bwd")
+
+
+# ---------------------------------------- norm and clipping of all gradients
+
+_KINDS = {"2": CBW_GRAD_NORM_2, "inf": CBW_GRAD_NORM_INF}
+
+
+def cbw_grad_workspace_size(grads):
+    return _bytes("cbw_grad_workspace_size", grads.array, len(grads))
+
+
+def grad_workspace(grads, device="cuda"):
+    """A uint8 device tensor of the size grad_norm and grad_clip need."""
+    return _workspace_of(cbw_grad_workspace_size(grads), device)
+
+
+def grad_norm(grads, norm, ws, kind="2", stream=None):
+    """norm[0] = the norm ("2" or "inf") of a GradList's tensors taken together."""
+    import torch
+    _check(lib().grad_norm(grads.array, len(grads), _KINDS[kind], _whole(norm, 1, torch.float32), _ptr(ws), _nbytes(ws),
+                           _stream(stream)), "grad_norm")
+
+
+def grad_clip(grads, max_norm, norm, ws, kind="2", stream=None):
+    """The GradList's outputs = its gradients times min(1, max_norm / (norm +
+    1e-6)); norm (float32, on the device) = the norm and that factor."""
+    import torch
+    _check(lib().grad_clip(grads.array, len(grads), _KINDS[kind], max_norm, _whole(norm, 2, torch.float32), _ptr(ws),
+                           _nbytes(ws), _stream(stream)), "grad_clip")
