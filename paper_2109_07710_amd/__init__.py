@@ -101,6 +101,10 @@ class NormParams(ctypes.Structure):
 
     def __init__(self, w_pre=None, b_pre=None, w_post=None, b_post=None, scale=None):
         self.tensors = (w_pre, b_pre, w_post, b_post, scale)
+        sizes = {t.numel() for t in self.tensors if t is not None}
+        if len(sizes) > 1:
+            raise ValueError("parameters of different sizes: %s" % sorted(sizes))
+        self.size = sizes.pop() if sizes else None
         super().__init__(*(None if t is None else _typed(t, CBW_F32).data_ptr() for t in self.tensors))
 
 
@@ -238,31 +242,46 @@ def _typed(t, dtype):
     return t
 
 
+_torch_types = None
+
+
+def _types():
+    """torch's types of the library's, and int32."""
+    global _torch_types
+    if _torch_types is None:
+        import torch
+        _torch_types = (torch.float32, torch.bfloat16, torch.int32)
+    return _torch_types
+
+
 def _rows(t, rows, cols, stride, dtype):
-    """Device pointer of a row tensor [rows][cols] of the given type whose
-    rows lie `stride` elements apart (None -> NULL)."""
+    """Device pointer of a row tensor [rows][cols] of the given torch type
+    whose rows lie `stride` elements apart (None -> NULL)."""
     if t is None:
         return None
+    if t.shape == (rows, cols) and t.dtype is dtype and t.is_cuda and t.stride() == (stride, 1):
+        return t.data_ptr()
+    # not the usual form: name what is wrong, or let pass where a stride has no meaning
     if not t.is_cuda:
         raise ValueError("expected a device tensor")
     if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
         raise ValueError("expected a tensor of shape (%d, %d), got %s" % (rows, cols, tuple(t.shape)))
+    if t.dtype is not dtype:
+        raise ValueError("expected a %s tensor, got %s" % (dtype, t.dtype))
     if rows > 0 and (t.stride(1) != 1 and cols > 1 or t.stride(0) != stride and rows > 1):
         raise ValueError("expected rows %d elements apart, got strides %s" % (stride, t.stride()))
-    if _dtype_of(t) != dtype:
-        raise ValueError("expected a %s tensor" % ("float32" if dtype == CBW_F32 else "bfloat16"))
     return t.data_ptr()
 
 
-def _whole(t, numel, torch_dtype):
+def _whole(t, numel, dtype):
     """Device pointer of a contiguous tensor of at least `numel` elements of
     the given torch type (None -> NULL)."""
     if t is None:
         return None
     if not t.is_cuda:
         raise ValueError("expected a device tensor")
-    if t.dtype != torch_dtype or t.numel() < numel or not t.is_contiguous():
-        raise ValueError("expected a contiguous %s tensor of %d elements" % (torch_dtype, numel))
+    if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous():
+        raise ValueError("expected a contiguous %s tensor of %d elements" % (dtype, numel))
     return t.data_ptr()
 
 
@@ -472,50 +491,41 @@ def expert_workspace(desc, device="cuda"):
     return _workspace_of(cbw_expert_workspace_size(desc), device)
 
 
-def _filters(d, W):
-    import torch
-    if tuple(W.shape) != (d.E, d.K, d.C):
+def _filters(d, W, dtype):
+    if W.shape != (d.E, d.K, d.C):
         raise ValueError("expected filters of shape (%d, %d, %d), got %s" % (d.E, d.K, d.C, tuple(W.shape)))
-    return _whole(W, d.E * d.K * d.C, torch.float32 if d.dtype == CBW_F32 else torch.bfloat16)
-
-
-def _offsets(d, offsets):
-    import torch
-    return _whole(offsets, d.E + 1, torch.int32)
+    return _whole(W, 0, dtype)
 
 
 def expert_fwd(desc, X, W, offsets, Y, y_mask, ws, flags=0, stream=None):
     """Y = X W[e]^T for the rows of every expert e, [offsets[e], offsets[e+1])
     (offsets: int32 on the device); CBW_FLAG_RELU: its ReLU, and y_mask its
     footprint bits (int32 words, or None)."""
-    import torch
-    d = desc
-    _check(lib().expert_fwd(ctypes.byref(d), _rows(X, d.rows, d.C, d.x_stride, d.dtype), _filters(d, W),
-                            _offsets(d, offsets), _rows(Y, d.rows, d.K, d.y_stride, d.dtype),
-                            _whole(y_mask, (d.rows * d.K + 31) // 32, torch.int32), _ptr(ws), _nbytes(ws), flags,
+    d, types = desc, _types()
+    dt, rows, C, K = types[d.dtype], d.rows, d.C, d.K
+    _check(lib().expert_fwd(ctypes.byref(d), _rows(X, rows, C, d.x_stride, dt), _filters(d, W, dt),
+                            _whole(offsets, d.E + 1, types[2]), _rows(Y, rows, K, d.y_stride, dt),
+                            _whole(y_mask, (rows * K + 31) // 32, types[2]), _ptr(ws), _nbytes(ws), flags,
                             _stream(stream)), "expert_fwd")
 
 
 def expert_bwd_data(desc, dY, W, offsets, x_mask, dX, ws, stream=None):
     """dX = dY W[e], +0.0 where x_mask (None: everywhere live) is dead."""
-    import torch
-    d = desc
-    _check(lib().expert_bwd_data(ctypes.byref(d), _rows(dY, d.rows, d.K, d.y_stride, d.dtype), _filters(d, W),
-                                 _offsets(d, offsets), _whole(x_mask, (d.rows * d.C + 31) // 32, torch.int32),
-                                 _rows(dX, d.rows, d.C, d.x_stride, d.dtype), _ptr(ws), _nbytes(ws), _stream(stream)),
+    d, types = desc, _types()
+    dt, rows, C, K = types[d.dtype], d.rows, d.C, d.K
+    _check(lib().expert_bwd_data(ctypes.byref(d), _rows(dY, rows, K, d.y_stride, dt), _filters(d, W, dt),
+                                 _whole(offsets, d.E + 1, types[2]), _whole(x_mask, (rows * C + 31) // 32, types[2]),
+                                 _rows(dX, rows, C, d.x_stride, dt), _ptr(ws), _nbytes(ws), _stream(stream)),
            "expert_bwd_data")
 
 
 def expert_bwd_weight(desc, X, dY, offsets, dW, ws, stream=None):
     """dW[e] = dY^T X over the rows of every expert e, float32 [E][K][C]."""
-    import torch
-    d = desc
-    if tuple(dW.shape) != (d.E, d.K, d.C):
-        raise ValueError("expected gradients of shape (%d, %d, %d), got %s" % (d.E, d.K, d.C, tuple(dW.shape)))
-    _check(lib().expert_bwd_weight(ctypes.byref(d), _rows(X, d.rows, d.C, d.x_stride, d.dtype),
-                                   _rows(dY, d.rows, d.K, d.y_stride, d.dtype), _offsets(d, offsets),
-                                   _whole(dW, d.E * d.K * d.C, torch.float32), _ptr(ws), _nbytes(ws), _stream(stream)),
-           "expert_bwd_weight")
+    d, types = desc, _types()
+    dt, rows, C, K = types[d.dtype], d.rows, d.C, d.K
+    _check(lib().expert_bwd_weight(ctypes.byref(d), _rows(X, rows, C, d.x_stride, dt), _rows(dY, rows, K, d.y_stride, dt),
+                                   _whole(offsets, d.E + 1, types[2]), _filters(d, dW, types[CBW_F32]), _ptr(ws),
+                                   _nbytes(ws), _stream(stream)), "expert_bwd_weight")
 
 
 # -------------------------------- norms around a block, gate, residual scale
@@ -536,38 +546,33 @@ def norm_workspace(desc, device="cuda"):
 def _params(p, C):
     if p is None:
         return None
-    for t in p.tensors:
-        if t is not None and t.numel() != C:
-            raise ValueError("expected parameters of %d values, got %d" % (C, t.numel()))
+    if p.size is not None and p.size != C:
+        raise ValueError("expected parameters of %d values, got %d" % (C, p.size))
     return ctypes.byref(p)
-
-
-def _gate(d, gate):
-    return _rows(gate, (d.rows + d.gate_rows - 1) // d.gate_rows, d.C, d.gate_stride, d.dtype)
 
 
 def block_norm_fwd(desc, x, u, gate, params, y, h, stats=None, stream=None):
     """y = x + scale * act(gate) * N_post(u), h = N_pre(y); u, gate and y None:
     h = N_pre(x).  stats (float32 [rows][4], or None): what the backward needs."""
-    import torch
-    d = desc
-    res = lambda t: _rows(t, d.rows, d.C, d.res_stride, d.res_dtype)  # noqa: E731
-    blk = lambda t: _rows(t, d.rows, d.C, d.block_stride, d.dtype)  # noqa: E731
-    _check(lib().block_norm_fwd(ctypes.byref(d), res(x), blk(u), _gate(d, gate), _params(params, d.C), res(y), blk(h),
-                                _whole(stats, 4 * d.rows, torch.float32), _stream(stream)), "block_norm_fwd")
+    d, types = desc, _types()
+    rows, C, rs, bs, rt, bt = d.rows, d.C, d.res_stride, d.block_stride, types[d.res_dtype], types[d.dtype]
+    _check(lib().block_norm_fwd(ctypes.byref(d), _rows(x, rows, C, rs, rt), _rows(u, rows, C, bs, bt),
+                                _rows(gate, -(-rows // d.gate_rows), C, d.gate_stride, bt), _params(params, C),
+                                _rows(y, rows, C, rs, rt), _rows(h, rows, C, bs, bt), _whole(stats, 4 * rows, types[CBW_F32]),
+                                _stream(stream)), "block_norm_fwd")
 
 
 def block_norm_bwd(desc, y, u, gate, params, stats, dy, dh, dx, du, dgate, grads, ws, stream=None):
     """The gradients of block_norm_fwd's inputs from dy and dh; dy, du, dgate
     and each of grads (a NormParams) may be None."""
-    import torch
-    d = desc
-    res = lambda t: _rows(t, d.rows, d.C, d.res_stride, d.res_dtype)  # noqa: E731
-    blk = lambda t: _rows(t, d.rows, d.C, d.block_stride, d.dtype)  # noqa: E731
-    _check(lib().block_norm_bwd(ctypes.byref(d), res(y), blk(u), _gate(d, gate), _params(params, d.C),
-                                _whole(stats, 4 * d.rows, torch.float32), res(dy), blk(dh), res(dx), blk(du),
-                                _gate(d, dgate), _params(grads, d.C), _ptr(ws), _nbytes(ws), _stream(stream)),
-           "block_norm_bwd")
+    d, types = desc, _types()
+    rows, C, rs, bs, rt, bt = d.rows, d.C, d.res_stride, d.block_stride, types[d.res_dtype], types[d.dtype]
+    gates, gs = -(-rows // d.gate_rows), d.gate_stride
+    _check(lib().block_norm_bwd(ctypes.byref(d), _rows(y, rows, C, rs, rt), _rows(u, rows, C, bs, bt),
+                                _rows(gate, gates, C, gs, bt), _params(params, C), _whole(stats, 4 * rows, types[CBW_F32]),
+                                _rows(dy, rows, C, rs, rt), _rows(dh, rows, C, bs, bt), _rows(dx, rows, C, rs, rt),
+                                _rows(du, rows, C, bs, bt), _rows(dgate, gates, C, gs, bt), _params(grads, C), _ptr(ws),
+                                _nbytes(ws), _stream(stream)), "block_norm_bwd")
 
 
 # ---------------------------------------- norm and clipping of all gradients
@@ -586,14 +591,12 @@ def grad_workspace(grads, device="cuda"):
 
 def grad_norm(grads, norm, ws, kind="2", stream=None):
     """norm[0] = the norm ("2" or "inf") of a GradList's tensors taken together."""
-    import torch
-    _check(lib().grad_norm(grads.array, len(grads), _KINDS[kind], _whole(norm, 1, torch.float32), _ptr(ws), _nbytes(ws),
-                           _stream(stream)), "grad_norm")
+    _check(lib().grad_norm(grads.array, len(grads.grads), _KINDS[kind], _whole(norm, 1, _types()[CBW_F32]), _ptr(ws),
+                           _nbytes(ws), _stream(stream)), "grad_norm")
 
 
 def grad_clip(grads, max_norm, norm, ws, kind="2", stream=None):
     """The GradList's outputs = its gradients times min(1, max_norm / (norm +
     1e-6)); norm (float32, on the device) = the norm and that factor."""
-    import torch
-    _check(lib().grad_clip(grads.array, len(grads), _KINDS[kind], max_norm, _whole(norm, 2, torch.float32), _ptr(ws),
-                           _nbytes(ws), _stream(stream)), "grad_clip")
+    _check(lib().grad_clip(grads.array, len(grads.grads), _KINDS[kind], max_norm, _whole(norm, 2, _types()[CBW_F32]),
+                           _ptr(ws), _nbytes(ws), _stream(stream)), "grad_clip")

@@ -41,64 +41,74 @@ __device__ __forceinline__ Group group_of(const ExpertArgs& a, int e)
     return {lo, hi - lo};
 }
 
+// Inclusive sum over the wave's lanes: shifts within rows of 16 lanes, then the
+// rows' totals carried on (register moves, no trip through the LDS).
 __device__ __forceinline__ int wave_inclusive_sum(int v)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int w = __shfl_up(v, o, 64);
-        if (lane >= o) v += w;
-    }
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // lane 15 of a row to the next one
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // lane 31 to the upper half
     return v;
 }
 
-// Units of work over the experts: units(e, group) each, numbered through.
-// Called by whole waves; every result is the same in all lanes.
+// The work of all experts, numbered through: expert e has units(e's group) of
+// it.  Up to 64 experts a lane keeps its expert's numbers; more are gone
+// through 64 at a time, again for every question.  Called by whole waves;
+// every result is the same in all lanes.
 template <typename F>
-__device__ __forceinline__ int count_units(const ExpertArgs& a, F units)
-{
-    int total = 0;
-    for (int e0 = 0; e0 < a.E; e0 += 64) {
-        const int e = e0 + (threadIdx.x & 63);
-        int n = e < a.E ? units(group_of(a, e)) : 0;
-        n = wave_inclusive_sum(n);
-        total += __builtin_amdgcn_readlane(n, 63);
-    }
-    return total;
-}
+struct Units {
+    const ExpertArgs& a;
+    F units;
+    int n, incl, total;   // of the lane's expert; of all
 
-// The expert that unit `u` belongs to, and its number within the expert.
-template <typename F>
-__device__ __forceinline__ int find_unit(const ExpertArgs& a, int u, F units, int& within)
-{
-    int before = 0;
-    for (int e0 = 0; e0 < a.E; e0 += 64) {
-        const int e = e0 + (threadIdx.x & 63);
-        const int n = e < a.E ? units(group_of(a, e)) : 0;
-        const int incl = before + wave_inclusive_sum(n);
-        const uint64_t m = __ballot(incl > u);
-        if (m != 0) {
-            const int at = __builtin_ctzll(m);
-            within = u - __builtin_amdgcn_readlane(incl - n, at);
-            return e0 + at;
+    __device__ Units(const ExpertArgs& args, F f) : a(args), units(f)
+    {
+        total = 0;
+        for (int e0 = 0; e0 < a.E; e0 += 64) {
+            load(e0, total);
+            total = __builtin_amdgcn_readlane(incl, 63);
         }
-        before = __builtin_amdgcn_readlane(incl, 63);
     }
-    within = 0;
-    return -1;
-}
+    __device__ void load(int e0, int before)
+    {
+        const int e = e0 + (threadIdx.x & 63);
+        n = e < a.E ? units(group_of(a, e)) : 0;
+        incl = before + wave_inclusive_sum(n);
+    }
+    // The expert that unit u belongs to, and its number within the expert.
+    __device__ int find(int u, int& within)
+    {
+        for (int e0 = 0, before = 0; e0 < a.E; e0 += 64) {
+            if (a.E > 64) load(e0, before);
+            const uint64_t m = __ballot(incl > u);
+            if (m != 0) {
+                const int at = __builtin_ctzll(m);
+                within = u - __builtin_amdgcn_readlane(incl - n, at);
+                return e0 + at;
+            }
+            before = __builtin_amdgcn_readlane(incl, 63);
+        }
+        within = 0;
+        return -1;
+    }
+};
+template <typename F>
+__device__ __forceinline__ Units<F> number_units(const ExpertArgs& a, F f) { return Units<F>(a, f); }
 
-// LDS placement of 16-byte chunks.  Along: rows of 128 bytes; a fragment read
-// takes one chunk of 16 consecutive rows per cycle, and rows of equal parity
-// share a half of the banks, so the chunk is moved by the row's bits 1 to 3.
-__device__ __forceinline__ int along_swizzle(int row) { return (row >> 1) & 7; }
-// Across, bf16: a transposing read takes 32 bytes of rows b .. b+3 and
-// b+8 .. b+11 per cycle: eight chunk pairs that must not share banks.
-__device__ __forceinline__ int across_swizzle(int row, uint16_t) { return 2 * ((row & 3) | (((row >> 3) & 1) << 2)); }
-// (tiles of 64 columns: rows of 128 bytes, of which two share the banks)
-__device__ __forceinline__ int across_swizzle_64(int row) { return 2 * (((row >> 1) & 1) | (((row >> 3) & 1) << 1)); }
-// Across, float32: a read takes 64 bytes of rows 4 apart per cycle.
-__device__ __forceinline__ int across_swizzle(int row, float) { return ((row >> 2) & 3) << 2; }
+// Waits until at most N of the wave's copies to LDS are in flight; the LDS reads
+// that follow stay behind it.
+template <int N>
+__device__ __forceinline__ void wait_copies()
+{
+    static_assert(N <= 63, "the counter's range");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// Until the wave's LDS reads have returned: what they read may be overwritten.
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint2 lds_read_transposed(const void* lds)
@@ -107,8 +117,8 @@ __device__ __forceinline__ uint2 lds_read_transposed(const void* lds)
     return __builtin_bit_cast(uint2, v);
 }
 
-// One operand tile in LDS: N columns (output features or rows) by KB
-// reduction indices, 128 * N bytes either way.
+// One operand tile in LDS: N columns (output features or rows) by 128 bytes of
+// reduction indices, filled by NW waves.
 template <typename T, int N, bool ACROSS, int NW>
 struct Operand {
     static constexpr int ESZ = sizeof(T), E = 16 / ESZ, KB = 128 / ESZ;
@@ -118,103 +128,136 @@ struct Operand {
     static constexpr int BYTES = N * 128;
     static_assert(COPIES >= 1 && LINES * CHUNKS % (64 * NW) == 0, "whole copies");
 
+    // Placement of the 16-byte chunks of an LDS row.  The LDS serves 256 bytes
+    // (all banks) a cycle.  Along: a fragment read takes one chunk of 16
+    // consecutive rows per cycle; with rows of 128 bytes, of which two share
+    // the banks, the chunk is moved by the row's bits 1 to 3, with rows of 64
+    // bytes by its bits 2 and 3.  Across, bf16: a transposing read takes 32
+    // bytes of rows b .. b+3 and b+8 .. b+11 per cycle: eight chunk pairs that
+    // must not share banks (tiles of 64 columns: rows of 128 bytes, two of
+    // them to the banks; of 32: four).  Across, float32: 64 bytes of rows 4 apart.
     static __device__ __forceinline__ int swizzle(int line)
     {
-        if (!ACROSS) return along_swizzle(line);
-        if (ESZ == 2 && N == 64) return across_swizzle_64(line);
-        return across_swizzle(line, T{});
+        if (!ACROSS) return (line >> 1) & 7;
+        if (ESZ == 4) return N >= 64 ? ((line >> 2) & 3) << 2 : ((line >> 2) & 1) << 2;
+        if (N >= 128) return 2 * ((line & 3) | (((line >> 3) & 1) << 2));
+        if (N == 64) return 2 * (((line >> 1) & 1) | (((line >> 3) & 1) << 1));
+        return 2 * ((line >> 3) & 1);
     }
 
     uint32_t off[COPIES];   // byte offset of the lane's 16 bytes at step 0, kOOB: never valid
-    int k0;                 // along: the lane's first reduction index at step 0
-    const char* base;       // (uniform) where offset 0 is
-    uint32_t bytes;
+    int k0[2];              // along: the lane's first reduction index at step 0, in even and odd copies
 
-    // along: `n` valid rows of `stride` elements from `p`, `len` reduction
-    // indices.  across: `n` valid columns from `p`, rows of `stride` elements.
-    __device__ void init(const void* p, int64_t n, int64_t stride)
+    // along: rows of `stride` elements; across: `n` valid columns
+    __device__ void init(int wave, int64_t n, int64_t stride)
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        base = static_cast<const char*>(p);
+        const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int j = 0; j < COPIES; ++j) {
             const int at = (wave + NW * j) * 64 + lane;
             const int line = at / CHUNKS, lc = (at % CHUNKS) ^ swizzle(line);
-            if (ACROSS) {
-                off[j] = lc * E < n ? (uint32_t)(line * stride + lc * E) * ESZ : kOOB;
-            } else {
-                off[j] = (uint32_t)(line * stride + lc * E) * ESZ;
-                k0 = lc * E;   // the same for every j: a wave's rows differ by multiples of 16
-            }
+            off[j] = ACROSS && lc * E >= n ? kOOB : (uint32_t)(line * stride + lc * E) * ESZ;
+            if (j < 2) k0[j] = lc * E;   // (two copies, 16 rows or more, further it is the same)
         }
-        static_assert(ACROSS || COPIES == 1 || NW % 2 == 0, "the lane's chunk is the same in every copy");
+        if (COPIES == 1) k0[1] = k0[0];
     }
 
     // Copy of a step's tile to LDS.  along: reduction indices from `k` on, of
     // `len`; across: the descriptor already starts at the step's first row.
-    __device__ __forceinline__ void copy(const u32x4_t& rsrc, int k, int len, uint4* lds) const
+    __device__ __forceinline__ void copy(int wave, const u32x4_t& rsrc, int k, int len, char* lds) const
     {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const uint32_t kill = ACROSS || k + k0 < len ? 0u : kOOB;
+        const uint32_t kill0 = ACROSS || k + k0[0] < len ? 0u : kOOB, kill1 = ACROSS || k + k0[1] < len ? 0u : kOOB;
 #pragma unroll
         for (int j = 0; j < COPIES; ++j)
-            buf_load16_lds(rsrc, ACROSS ? off[j] : (off[j] + (uint32_t)k * ESZ) | kill, lds_addr(lds + (wave + NW * j) * 64));
+            buf_load16_lds(rsrc, ACROSS ? off[j] : (off[j] + (uint32_t)k * ESZ) | (j & 1 ? kill1 : kill0),
+                           lds_addr(lds + (wave + NW * j) * 1024));
+    }
+
+    // The 16-wide fragment of columns cb .. cb+15 at the ks-th 64-byte part of
+    // a step (32 bf16 or 16 float32 reduction indices).
+    static __device__ __forceinline__ uint4 fragment(const char* lds, int cb, int ks)
+    {
+        const int lane = threadIdx.x & 63;
+        if (!ACROSS) {
+            const int row = cb + (lane & 15);
+            return *reinterpret_cast<const uint4*>(lds + row * 128 + (((ks * 4 + (lane >> 4)) ^ swizzle(row)) << 4));
+        }
+        if (ESZ == 2) {
+            const int line = ks * 32 + 8 * (lane >> 4) + ((lane >> 2) & 3), col = cb + 4 * (lane & 3);
+            auto at = [&](int r) { return lds + r * (N * 2) + (((col >> 3) ^ swizzle(r)) << 4) + ((col & 7) << 1); };
+            const uint2 lo = lds_read_transposed(at(line)), hi = lds_read_transposed(at(line + 4));
+            return make_uint4(lo.x, lo.y, hi.x, hi.y);
+        }
+        const int line = ks * 16 + 4 * (lane >> 4), col = cb + (lane & 15);
+        auto at = [&](int r) {
+            return *reinterpret_cast<const uint32_t*>(lds + r * (N * 4) + (((col >> 2) ^ swizzle(r)) << 4) + ((col & 3) << 2));
+        };
+        return make_uint4(at(line), at(line + 1), at(line + 2), at(line + 3));
     }
 };
 
-// The 16-wide fragment of columns cb .. cb+15 at the ks-th 64-byte part of a
-// step (32 bf16 or 16 float32 reduction indices).
-template <typename T, int N, bool ACROSS, int NW>
-__device__ __forceinline__ uint4 fragment(const char* lds, int cb, int ks)
-{
-    using O = Operand<T, N, ACROSS, NW>;
-    const int lane = threadIdx.x & 63;
-    if (!ACROSS) {
-        const int row = cb + (lane & 15);
-        return *reinterpret_cast<const uint4*>(lds + row * 128 + (((ks * 4 + (lane >> 4)) ^ O::swizzle(row)) << 4));
-    }
-    if (sizeof(T) == 2) {
-        const int line = ks * 32 + 8 * (lane >> 4) + ((lane >> 2) & 3), col = cb + 4 * (lane & 3);
-        auto at = [&](int r) { return lds + r * (N * 2) + (((col >> 3) ^ O::swizzle(r)) << 4) + ((col & 7) << 1); };
-        const uint2 lo = lds_read_transposed(at(line)), hi = lds_read_transposed(at(line + 4));
-        return make_uint4(lo.x, lo.y, hi.x, hi.y);
-    }
-    const int line = ks * 16 + 4 * (lane >> 4), col = cb + (lane & 15);
-    auto at = [&](int r) {
-        return *reinterpret_cast<const uint32_t*>(lds + r * (N * 4) + (((col >> 2) ^ O::swizzle(r)) << 4) + ((col & 3) << 2));
-    };
-    return make_uint4(at(line), at(line + 1), at(line + 2), at(line + 3));
-}
+// Output of the forward product and the data gradient: rows of P features,
+// `stride` elements apart, a tile's first row at offset 0.
+template <typename T, int KIND>
+struct Output {
+    const ExpertArgs& a;
+    __amdgpu_buffer_rsrc_t r;
+    int64_t row0, stride;
+    int rows, P;
 
-// Four consecutive output features of one row.
-__device__ __forceinline__ void store_features(__amdgpu_buffer_rsrc_t r, uint32_t elem, bool ok, const floatx4& v, uint16_t)
-{
-    const u32x2 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-    __builtin_amdgcn_raw_buffer_store_b64(w, r, ok ? elem * 2u : kOOB, 0, 0);
-}
-__device__ __forceinline__ void store_features(__amdgpu_buffer_rsrc_t r, uint32_t elem, bool ok, const floatx4& v, float)
-{
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, ok ? elem * 4u : kOOB, 0, 0);
-}
+    __device__ Output(const ExpertArgs& args, int64_t first, int n)
+        : a(args), row0(first), stride(KIND == FWD ? args.y_stride : args.x_stride), rows(n), P(KIND == FWD ? args.K : args.C)
+    {
+        r = make_rsrc(static_cast<T*>(a.out) + row0 * stride, (uint32_t)(((rows - 1) * stride + P) * (int64_t)sizeof(T)));
+    }
 
-// Where a tile of rows lies: expert, first row, rows.
-struct RowTile {
-    int expert;
-    int64_t row0;
-    int rows;
+    // Four features from p on of the tile's row q; the bits of those above
+    // zero as they are stored (the forward's footprint).
+    __device__ __forceinline__ uint32_t put(int q, int p, floatx4 v) const
+    {
+        const bool ok = q < rows && p < P;
+        if (KIND == FWD && a.relu)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = v[c] > 0.f ? v[c] : 0.f;
+        if (KIND == DATA && a.mask && ok) {
+            const int64_t bit = (row0 + q) * (int64_t)P + p;
+            const uint32_t m = reinterpret_cast<const uint8_t*>(a.mask)[bit >> 3] >> (bit & 7);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = (m >> c) & 1u ? v[c] : 0.f;
+        }
+        const uint32_t off = ok ? (uint32_t)(q * stride + p) * (uint32_t)sizeof(T) : kOOB;
+        if (sizeof(T) == 4) {
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, off, 0, 0);
+            return KIND == FWD ? (v[0] > 0.f) | (v[1] > 0.f) << 1 | (v[2] > 0.f) << 2 | (v[3] > 0.f) << 3 : 0;
+        }
+        const u32x2 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        __builtin_amdgcn_raw_buffer_store_b64(w, r, off, 0, 0);
+        // (after ReLU a stored value is positive unless its bits are zero)
+        return KIND == FWD ? ((w.x & 0xffffu) != 0) | ((w.x >> 16) != 0) << 1 | ((w.y & 0xffffu) != 0) << 2 | ((w.y >> 16) != 0) << 3 : 0;
+    }
+
+    // Footprint word of the 32 features from p on of row q, from the lanes'
+    // four bits of its two blocks of 16 features.
+    __device__ __forceinline__ void put_bits(int q, int p, uint32_t lo, uint32_t hi) const
+    {
+        uint32_t w = (lo | hi << 16) << (4 * ((threadIdx.x & 63) >> 4));
+        w |= __shfl_xor(w, 16);
+        w |= __shfl_xor(w, 32);
+        if ((threadIdx.x & 63) < 16 && q < rows && p < P) a.out_mask[((row0 + q) * (int64_t)P + p) >> 5] = w;
+    }
 };
 
 // TP x TQ output tile by NWP x NWQ waves, two buffers of a 128-byte step of
-// both operands, the next step's copies in flight during this one's products.
+// both operands.
 template <typename T, int KIND, int TP, int TQ, int NWP, int NWQ>
 __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
 {
     constexpr int NW = NWP * NWQ, FM = TP / NWP / 16, FN = TQ / NWQ / 16;
     using OP = Operand<T, TP, KIND != FWD, NW>;
     using OQ = Operand<T, TQ, KIND == WEIGHT, NW>;
-    constexpr int KB = OP::KB;
-    __shared__ uint4 lds_p[2][OP::BYTES / 16];
-    __shared__ uint4 lds_q[2][OQ::BYTES / 16];
+    constexpr int KB = OP::KB, COPIES = OP::COPIES + OQ::COPIES;
+    __shared__ __align__(1024) char lds_p[2][OP::BYTES];
+    __shared__ __align__(1024) char lds_q[2][OQ::BYTES];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wp = wave / NWQ, wq = wave % NWQ;
@@ -222,31 +265,37 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
     // the workgroup's tile
     const int P = KIND == FWD ? a.K : a.C;                     // features of the output
     const int ptiles = (P + TP - 1) / TP, qtiles = KIND == WEIGHT ? (a.K + TQ - 1) / TQ : 1;
-    auto units = [&](const Group& g) -> int {
-        if (KIND == WEIGHT) return (int)max((g.count + a.split_rows - 1) / a.split_rows, (int64_t)1);
-        return (int)((g.count + TQ - 1) / TQ);
-    };
-    const int nunits = count_units(a, units);
-    const int per = ptiles * qtiles, total = nunits * per;
-    if ((int)blockIdx.x >= total) return;
-    const int b = xcd_remap(blockIdx.x, total);
-    int unit, pt, qt = 0;
+    int unit, pt, qt = 0, within, e;
     if (KIND == WEIGHT) {
-        unit = b / per;
-        const int t = b - unit * per;
-        qt = t / ptiles;
-        pt = t - qt * ptiles;
+        // Units are experts, or parts of one, of very different lengths: every
+        // XCD takes an equal share of the tiles of each (contiguous, so that
+        // they share operands), the shares turning from unit to unit.
+        const int per = ptiles * qtiles, share = (per + 7) >> 3;
+        const int j = blockIdx.x >> 3;
+        unit = j / share;
+        const int t = (((int)blockIdx.x + unit) & 7) * share + j - unit * share;
+        if (t >= per) return;
+        pt = t / qtiles;
+        qt = t - pt * qtiles;
+        auto parts = [&](const Group& g) { return (int)max((g.count + a.split_rows - 1) / a.split_rows, (int64_t)1); };
+        e = number_units(a, parts).find(unit, within);
     } else {
-        // blocks of a few row tiles by all feature tiles, so that the tiles
-        // that run at one time share both operands in the cache
-        constexpr int GR = 4;
+        auto units = [&](const Group& g) { return (int)((g.count + TQ - 1) / TQ); };
+        auto all = number_units(a, units);
+        const int nunits = all.total, total = nunits * ptiles;
+        if ((int)blockIdx.x >= total) return;
+        const int b = xcd_remap(blockIdx.x, total);
+        // blocks of eight row tiles by all feature tiles, so that the tiles
+        // that run at one time share both operands in the cache (four: 2 to
+        // 10% slower at 16384 rows, 2048 -> 8192 features, 8 experts)
+        constexpr int GR = 8;
         const int blk = b / (GR * ptiles), in_blk = b - blk * GR * ptiles;
         const int h = min(GR, nunits - blk * GR);
         pt = in_blk / h;
         unit = blk * GR + in_blk - pt * h;
+        e = all.find(unit, within);
     }
-    int within;
-    const int e = __builtin_amdgcn_readfirstlane(find_unit(a, unit, units, within));
+    e = __builtin_amdgcn_readfirstlane(e);
     if (e < 0) return;
     const Group g = group_of(a, e);
     within = __builtin_amdgcn_readfirstlane(within);
@@ -257,42 +306,44 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
     int64_t row0 = 0;       // first row of the tile (weight: of the part)
     int64_t len;            // reduction indices
     int64_t qrows = 0;
+    const char *base_p, *base_q;
     if (KIND == WEIGHT) {
         row0 = g.first + (int64_t)within * a.split_rows;
         len = min((int64_t)a.split_rows, g.first + g.count - row0);
-        op.init(static_cast<const T*>(a.p) + row0 * a.x_stride + p0, a.C - p0, a.x_stride);
-        oq.init(static_cast<const T*>(a.q) + row0 * a.y_stride + q0, a.K - q0, a.y_stride);
+        base_p = reinterpret_cast<const char*>(static_cast<const T*>(a.p) + row0 * a.x_stride + p0);
+        base_q = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + row0 * a.y_stride + q0);
+        op.init(wave, a.C - p0, a.x_stride);
+        oq.init(wave, a.K - q0, a.y_stride);
     } else {
         const int64_t qstride = KIND == FWD ? a.x_stride : a.y_stride;
         const T* w = static_cast<const T*>(a.p) + (int64_t)e * a.K * a.C;
         row0 = g.first + (int64_t)within * TQ;
         qrows = min((int64_t)TQ, g.first + g.count - row0);
         len = KIND == FWD ? a.C : a.K;
-        if (KIND == FWD) op.init(w + (int64_t)p0 * a.C, min(TP, a.K - p0), a.C);
-        else op.init(w + p0, a.C - p0, a.C);
-        oq.init(static_cast<const T*>(a.q) + row0 * qstride, qrows, qstride);
+        base_p = reinterpret_cast<const char*>(w + (KIND == FWD ? (int64_t)p0 * a.C : (int64_t)p0));
+        base_q = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + row0 * qstride);
+        op.init(wave, KIND == FWD ? 0 : a.C - p0, a.C);
+        oq.init(wave, 0, qstride);
     }
 
     auto copy = [&](int64_t k, int buf) {
-        // P
+        const int64_t left = min(len - k, (int64_t)KB);
+        // (an operand that goes across: the step's rows, the last of which ends with its own columns)
         if (KIND == FWD) {
             const uint32_t n = (uint32_t)min(TP, a.K - p0) * (uint32_t)a.C * sizeof(T);
-            op.copy(make_rsrc_words(op.base, n), (int)k, (int)len, lds_p[buf]);
+            op.copy(wave, make_rsrc_words(base_p, n), (int)k, (int)len, lds_p[buf]);
         } else {
             const int64_t stride = KIND == WEIGHT ? a.x_stride : (int64_t)a.C;
-            const int64_t left = min(len - k, (int64_t)KB);
-            // the last row ends with its own columns
             const uint32_t n = (uint32_t)(((left - 1) * stride + a.C - p0) * (int64_t)sizeof(T));
-            op.copy(make_rsrc_words(op.base + k * stride * (int64_t)sizeof(T), n), 0, 0, lds_p[buf]);
+            op.copy(wave, make_rsrc_words(base_p + k * stride * (int64_t)sizeof(T), n), 0, 0, lds_p[buf]);
         }
         if (KIND == WEIGHT) {
-            const int64_t left = min(len - k, (int64_t)KB);
             const uint32_t n = (uint32_t)(((left - 1) * a.y_stride + a.K - q0) * (int64_t)sizeof(T));
-            oq.copy(make_rsrc_words(oq.base + k * a.y_stride * (int64_t)sizeof(T), n), 0, 0, lds_q[buf]);
+            oq.copy(wave, make_rsrc_words(base_q + k * a.y_stride * (int64_t)sizeof(T), n), 0, 0, lds_q[buf]);
         } else {
             const int64_t stride = KIND == FWD ? a.x_stride : a.y_stride;
             const uint32_t n = (uint32_t)(((qrows - 1) * stride + len) * (int64_t)sizeof(T));
-            oq.copy(make_rsrc_words(oq.base, n), (int)k, (int)len, lds_q[buf]);
+            oq.copy(wave, make_rsrc_words(base_q, n), (int)k, (int)len, lds_q[buf]);
         }
     };
 
@@ -302,42 +353,72 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-    const int64_t steps = (len + KB - 1) / KB;
+    // Fragments of a step's two halves in turn: while the matrix instructions of
+    // one run, the reads of the next are under way, so that the LDS latency is
+    // under them and not behind the barrier.  The barrier stands between the
+    // halves: there every wave holds the step's second half in registers, the
+    // buffer is free for the copies two steps ahead, and the next step's have
+    // landed.
+    struct Fragments {
+        uint4 p[FM], q[FN];
+    };
+    auto read = [&](Fragments& f, int buf, int ks) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) f.q[j] = OQ::fragment(lds_q[buf], wq * (TQ / NWQ) + j * 16, ks);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) f.p[i] = OP::fragment(lds_p[buf], wp * (TP / NWP) + i * 16, ks);
+    };
+    auto multiply = [&](const Fragments& f) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = mfma_chunk(acc[i][j], f.p[i], f.q[j], T{});
+    };
+    // one or two reads between every few matrix instructions
+    auto interleave = [&]() {
+        constexpr int READS = (FM * (KIND != FWD ? 2 : 1) + FN * (KIND == WEIGHT ? 2 : 1)), MUL = FM * FN;
+        if (sizeof(T) != 2) return;
+#pragma unroll
+        for (int i = 0; i < READS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                    // an LDS read
+            __builtin_amdgcn_sched_group_barrier(0x008, MUL / READS, 0);          // matrix instructions
+        }
+    };
+    const int steps = (int)((len + KB - 1) / KB);
+    Fragments fa, fb;
     if (steps > 0) {
         copy(0, 0);
-        wait_vmem();
-        __syncthreads();
-    }
-    for (int64_t s = 0; s < steps; ++s) {
-        const int buf = (int)(s & 1);
-        if (s + 1 < steps) copy((s + 1) * KB, buf ^ 1);
-        const char* lp = reinterpret_cast<const char*>(lds_p[buf]);
-        const char* lq = reinterpret_cast<const char*>(lds_q[buf]);
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            uint4 fp[FM], fq[FN];
-#pragma unroll
-            for (int i = 0; i < FM; ++i) fp[i] = fragment<T, TP, KIND != FWD, NW>(lp, wp * (TP / NWP) + i * 16, ks);
-#pragma unroll
-            for (int j = 0; j < FN; ++j) fq[j] = fragment<T, TQ, KIND == WEIGHT, NW>(lq, wq * (TQ / NWQ) + j * 16, ks);
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = mfma_chunk(acc[i][j], fp[i], fq[j], T{});
+        if (steps > 1) {
+            copy(KB, 1);
+            wait_copies<COPIES>();
+        } else {
+            wait_copies<0>();
         }
-        wait_vmem();
-        __syncthreads();
+        barrier();
+        read(fa, 0, 0);
+    }
+    for (int s = 0; s < steps; ++s) {
+        const int buf = s & 1;
+        read(fb, buf, 1);
+        multiply(fa);
+        interleave();
+        wait_copies<0>();
+        wait_reads();
+        barrier();
+        if (s + 2 < steps) copy((int64_t)(s + 2) * KB, buf);
+        read(fa, buf ^ 1, 0);   // (after the last step: what was there, unused)
+        multiply(fb);
+        interleave();
     }
 
     const int pl = p0 + wp * (TP / NWP) + 4 * (lane >> 4), ql = wq * (TQ / NWQ) + (lane & 15);
     if (KIND == WEIGHT) {
         float* out = nullptr;
-        auto slots = [&](const Group& gg) -> int {
-            const int n = units(gg);
-            return n > 1 ? n : 0;
-        };
-        if (units(g) > 1) {
+        if (g.count > a.split_rows) {
             // the expert's slots follow those of the split experts before it
+            auto slots = [&](const Group& gg) {
+                return gg.count > a.split_rows ? (int)((gg.count + a.split_rows - 1) / a.split_rows) : 0;
+            };
             int before = 0;
             for (int e0 = 0; e0 < e; e0 += 64) {
                 const int x = e0 + lane;
@@ -352,54 +433,140 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
         for (int j = 0; j < FN; ++j) {
             const int k = q0 + ql + j * 16;
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
-                store_features(r, (uint32_t)k * (uint32_t)a.C + pl + i * 16, k < a.K && pl + i * 16 < a.C, acc[i][j], 0.f);
+            for (int i = 0; i < FM; ++i) {
+                // non-temporal: the gradients are not read again here, and as
+                // ordinary stores they push the operands out of the L2 (64
+                // experts of 512 rows on average, 2048 -> 1408: 385 us, 323 so)
+                const uint32_t off = k < a.K && pl + i * 16 < a.C ? ((uint32_t)k * (uint32_t)a.C + pl + i * 16) * 4u : kOOB;
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), r, off, 0, 2);
+            }
         }
         return;
     }
-    const int64_t ostride = KIND == FWD ? a.y_stride : a.x_stride;
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(static_cast<T*>(a.out) + row0 * ostride,
-                                               (uint32_t)(((qrows - 1) * ostride + P) * (int64_t)sizeof(T)));
+    const Output<T, KIND> out(a, row0, (int)qrows);
+    const bool bits = KIND == FWD && a.out_mask;
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-        const int q = ql + j * 16;
-        const bool row_in = q < qrows;
-        uint32_t bits16 = 0;
+    for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int p = pl + i * 16;
-            floatx4 v = acc[i][j];
-            if (KIND == FWD && a.relu)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] = v[c] > 0.f ? v[c] : 0.f;
-            if (KIND == DATA && a.mask && row_in && p < P) {
-                const int64_t bit = (row0 + q) * (int64_t)P + p;
-                const uint32_t m = reinterpret_cast<const uint8_t*>(a.mask)[bit >> 3] >> (bit & 7);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] = (m >> c) & 1u ? v[c] : 0.f;
-            }
-            store_features(r, (uint32_t)(q * ostride + p), row_in && p < P, v, T{});
-            if (KIND == FWD && a.out_mask) {
-                // the footprint of what is stored (a sum below the smallest bf16 rounds to zero); the four lane groups' nibbles
-                // make 16 bits, two blocks a word
-                uint32_t nib = 0;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const float s = sizeof(T) == 2 ? __uint_as_float(f32_to_bf16_rne(v[c]) << 16) : v[c];
-                    nib |= (s > 0.f ? 1u : 0u) << c;
-                }
-                nib <<= 4 * (lane >> 4);
-                nib |= __shfl_xor(nib, 16);
-                nib |= __shfl_xor(nib, 32);
-                if (i & 1) {
-                    const int pw = p0 + wp * (TP / NWP) + (i - 1) * 16;   // a multiple of 32
-                    if (lane < 16 && row_in && pw < P)
-                        a.out_mask[((row0 + q) * (int64_t)P + pw) >> 5] = bits16 | (nib << 16);
-                } else {
-                    bits16 = nib;
-                }
-            }
+        for (int i = 0; i < FM; i += 2) {
+            const uint32_t lo = out.put(ql + j * 16, pl + i * 16, acc[i][j]);
+            const uint32_t hi = out.put(ql + j * 16, pl + i * 16 + 16, acc[i + 1][j]);
+            if (bits) out.put_bits(ql + j * 16, p0 + wp * (TP / NWP) + i * 16, lo, hi);
         }
+}
+
+// Few rows to an expert (serving, or many experts): bound by reading the
+// filters.  A workgroup takes TP features by 16 FN rows and its waves share out
+// the reduction, each streaming its own steps through a ring of its own in LDS
+// without a barrier, so that a CU has all its waves' copies in flight; the
+// waves' sums are added in order at the end.
+template <typename T, int KIND, int TP, int FN, int NW, int RING>
+__global__ __launch_bounds__(NW * 64) void expert_stream_kernel(ExpertArgs a)
+{
+    constexpr int TQ = 16 * FN, FM = TP / 16;
+    using OP = Operand<T, TP, KIND != FWD, 1>;
+    using OQ = Operand<T, TQ, false, 1>;
+    constexpr int KB = OP::KB, COPIES = OP::COPIES + OQ::COPIES, STAGE = OP::BYTES + OQ::BYTES;
+    constexpr int SUMS = NW * FM * FN * 1024;
+    __shared__ __align__(1024) char lds[NW * RING * STAGE > SUMS ? NW * RING * STAGE : SUMS];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int P = KIND == FWD ? a.K : a.C, ptiles = (P + TP - 1) / TP;
+    auto all = number_units(a, [&](const Group& g) { return (int)((g.count + TQ - 1) / TQ); });
+    const int nunits = all.total, total = nunits * ptiles;
+    if ((int)blockIdx.x >= total) return;
+    // as in the tiled kernel: row tiles of one expert meet in one XCD
+    constexpr int GR = 8;
+    const int b = xcd_remap(blockIdx.x, total);
+    const int blk = b / (GR * ptiles), in_blk = b - blk * GR * ptiles;
+    const int h = min(GR, nunits - blk * GR);
+    const int pt = in_blk / h;
+    int within;
+    const int e = __builtin_amdgcn_readfirstlane(all.find(blk * GR + in_blk - pt * h, within));
+    if (e < 0) return;
+    const Group g = group_of(a, e);
+    within = __builtin_amdgcn_readfirstlane(within);
+    const int p0 = pt * TP;
+    const int64_t row0 = g.first + (int64_t)within * TQ;
+    const int qrows = (int)min((int64_t)TQ, g.first + g.count - row0);
+    const int64_t qstride = KIND == FWD ? a.x_stride : a.y_stride;
+    const int len = KIND == FWD ? a.C : a.K;
+    const T* w = static_cast<const T*>(a.p) + (int64_t)e * a.K * a.C;
+    const char* base_p = reinterpret_cast<const char*>(w + (KIND == FWD ? (int64_t)p0 * a.C : (int64_t)p0));
+    const char* base_q = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + row0 * qstride);
+    const u32x4_t rq = make_rsrc_words(base_q, (uint32_t)(((qrows - 1) * qstride + len) * (int64_t)sizeof(T)));
+    OP op;
+    OQ oq;
+    op.init(0, KIND == FWD ? 0 : a.C - p0, a.C);
+    oq.init(0, 0, qstride);
+    char* ring = lds + wave * RING * STAGE;
+
+    auto copy = [&](int step, int slot) {
+        const int64_t k = (int64_t)step * KB;
+        if (KIND == FWD) {
+            const uint32_t n = (uint32_t)min(TP, a.K - p0) * (uint32_t)a.C * sizeof(T);
+            op.copy(0, make_rsrc_words(base_p, n), (int)k, len, ring + slot * STAGE);
+        } else {
+            const int64_t left = min(len - k, (int64_t)KB);
+            const uint32_t n = (uint32_t)(((left - 1) * a.C + a.C - p0) * (int64_t)sizeof(T));
+            op.copy(0, make_rsrc_words(base_p + k * a.C * (int64_t)sizeof(T), n), 0, 0, ring + slot * STAGE);
+        }
+        oq.copy(0, rq, (int)k, len, ring + slot * STAGE + OP::BYTES);
+    };
+
+    floatx4 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+    // this wave's steps: wave, wave + NW, ...
+    const int steps = ((len + KB - 1) / KB - wave + NW - 1) / NW;
+#pragma unroll
+    for (int t = 0; t < RING; ++t)
+        if (t < steps) copy(wave + t * NW, t);
+    int slot = 0;
+    for (int t = 0; t < steps; ++t) {
+        if (t + RING <= steps) wait_copies<(RING - 1) * COPIES>();
+        else wait_copies<0>();
+        const char *lp = ring + slot * STAGE, *lq = lp + OP::BYTES;
+        uint4 fp[2][FM], fq[2][FN];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) fq[ks][j] = OQ::fragment(lq, j * 16, ks);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) fp[ks][i] = OP::fragment(lp, i * 16, ks);
+        }
+        wait_reads();
+        if (t + RING < steps) copy(wave + (t + RING) * NW, slot);
+        slot = slot == RING - 1 ? 0 : slot + 1;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = mfma_chunk(acc[i][j], fp[ks][i], fq[ks][j], T{});
+    }
+
+    __syncthreads();   // every wave is done with its ring
+    floatx4* sums = reinterpret_cast<floatx4*>(lds);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) sums[(wave * FM * FN + i * FN + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    const Output<T, KIND> out(a, row0, qrows);
+    for (int u = wave; u < FM / 2 * FN; u += NW) {
+        const int i = u / FN * 2, j = u % FN;
+        floatx4 v[2] = {};
+#pragma unroll
+        for (int z = 0; z < NW; ++z)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) v[k] += sums[(z * FM * FN + (i + k) * FN + j) * 64 + lane];
+        const int q = j * 16 + (lane & 15), p = p0 + i * 16 + 4 * (lane >> 4);
+        const uint32_t lo = out.put(q, p, v[0]), hi = out.put(q, p + 16, v[1]);
+        if (KIND == FWD && a.out_mask) out.put_bits(q, p0 + i * 16, lo, hi);
     }
 }
 
@@ -437,21 +604,69 @@ hipError_t launch_tiles(const ExpertArgs& a, hipStream_t s)
 {
     const int P = KIND == FWD ? a.K : a.C;
     const int64_t per = (int64_t)((P + TP - 1) / TP) * (KIND == WEIGHT ? (a.K + TQ - 1) / TQ : 1);
-    const int64_t units = KIND == WEIGHT ? a.rows / a.split_rows + a.E : most_units(a.rows, a.E, TQ);
-    if (units == 0) return hipSuccess;
-    if (units * per > 0x7fffffff) return hipErrorInvalidValue;
-    expert_kernel<T, KIND, TP, TQ, NWP, NWQ><<<(int)(units * per), NWP * NWQ * 64, 0, s>>>(a);
+    const int64_t grid = KIND == WEIGHT ? (a.rows / a.split_rows + a.E) * ((per + 7) / 8 * 8) : most_units(a.rows, a.E, TQ) * per;
+    if (grid == 0) return hipSuccess;
+    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    expert_kernel<T, KIND, TP, TQ, NWP, NWQ><<<(int)grid, NWP * NWQ * 64, 0, s>>>(a);
     return hipGetLastError();
+}
+
+template <typename T, int KIND, int TP, int FN, int NW, int RING>
+hipError_t launch_stream(const ExpertArgs& a, hipStream_t s)
+{
+    const int P = KIND == FWD ? a.K : a.C;
+    const int64_t grid = most_units(a.rows, a.E, 16 * FN) * ((P + TP - 1) / TP);
+    if (grid == 0) return hipSuccess;
+    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    expert_stream_kernel<T, KIND, TP, FN, NW, RING><<<(int)grid, NW * 64, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+// Tiles of `tile` rows by `width` features, the rows spread evenly over the
+// experts (the host does not know the lengths).
+int64_t likely_tiles(const ExpertArgs& a, int tile, int P, int width)
+{
+    const int64_t busy = std::max<int64_t>(1, std::min<int64_t>(a.E, a.rows)), mean = (a.rows + busy - 1) / busy;
+    return busy * ((mean + tile - 1) / tile) * ((P + width - 1) / width);
+}
+
+// Forward product and data gradient.  Large tiles need the fewest bytes from
+// the caches but rows enough to fill them and tiles enough to fill the chip;
+// where there are neither, the streaming kernel splits the reduction over its
+// waves.  Measured (us, bf16, forward; 256 x 256 | 128 x 128 | stream, 16 rows |
+// stream, 64 rows): 16384 rows, 8 experts, 2048 -> 8192: 536 | 700 | - | -;
+// 6935 rows, 36 experts, 1736 -> 1312: 56 | 68 | 145 | 107; 3676, 3, 264 ->
+// 1576: 17 | 13 | 37 | 28; 256, 8, 2048 -> 8192: 54 | 44 | 53 | 55; 755, 1, 2664
+// -> 536: 59 | 38 | 14 | 13; 2108, 46, 848 -> 152: 22 | 13 | 7 | 8; 12, 32, 2048
+// -> 1408: 43 | 24 | 12 | 13.  Few tiles of 64 features: 16 rows, 1 expert, 8192
+// -> 512: 17, and 10 with 32 features and eight waves.
+template <typename T, int KIND>
+hipError_t launch_rows(const ExpertArgs& a, hipStream_t s)
+{
+    constexpr bool BF16 = sizeof(T) == 2;
+    const int P = KIND == FWD ? a.K : a.C;
+    const int64_t mean = a.rows / std::max<int64_t>(1, std::min<int64_t>(a.E, a.rows));
+    if constexpr (BF16) {
+        if (mean >= 160 && likely_tiles(a, 256, P, 256) >= 200) return launch_tiles<T, KIND, 256, 256, 2, 4>(a, s);
+        if (mean > 16 && likely_tiles(a, 128, P, 128) >= 200) return launch_tiles<T, KIND, 128, 128, 2, 2>(a, s);
+    } else {
+        if (mean > 16 && likely_tiles(a, 64, P, 64) >= 400) return launch_tiles<T, KIND, 64, 64, 2, 2>(a, s);
+    }
+    if (mean > 64) return launch_stream<T, KIND, 64, 4, 4, 2>(a, s);
+    if (likely_tiles(a, 16, P, 64) >= 192) return launch_stream<T, KIND, 64, 1, 4, 2>(a, s);
+    return launch_stream<T, KIND, 32, 1, 8, 3>(a, s);
 }
 
 }  // namespace
 
+// Parts long enough that their sums' way through memory stays small beside
+// the products, and short enough that there are about two tiles for a CU.
 ExpertPlan expert_plan(const cbw_expert_desc* d)
 {
     ExpertPlan p{};
-    const int64_t tiles = (int64_t)((d->C + 255) / 256) * ((d->K + 255) / 256);
-    int64_t len = d->rows * tiles / 1024;
-    len = std::max<int64_t>(1024, (len + 63) / 64 * 64);
+    const int side = d->dtype == CBW_F32 ? 64 : 256;
+    const int64_t tiles = (int64_t)((d->C + side - 1) / side) * ((d->K + side - 1) / side);
+    const int64_t len = std::max<int64_t>(512, (d->rows * tiles / 512 + 63) / 64 * 64);
     p.split_rows = (int)std::min<int64_t>(len, 1 << 30);
     p.slots = d->rows > p.split_rows ? 2 * d->rows / p.split_rows : 0;
     p.ws_bytes = (size_t)p.slots * d->K * d->C * 4;
@@ -460,22 +675,28 @@ ExpertPlan expert_plan(const cbw_expert_desc* d)
 
 hipError_t launch_expert_fwd(int dtype, const ExpertArgs& a, hipStream_t s)
 {
-    if (dtype == CBW_F32) return launch_tiles<float, FWD, 64, 64, 2, 2>(a, s);
-    return launch_tiles<uint16_t, FWD, 256, 256, 2, 4>(a, s);
+    return dtype == CBW_F32 ? launch_rows<float, FWD>(a, s) : launch_rows<uint16_t, FWD>(a, s);
 }
 
 hipError_t launch_expert_bwd_data(int dtype, const ExpertArgs& a, hipStream_t s)
 {
-    if (dtype == CBW_F32) return launch_tiles<float, DATA, 64, 64, 2, 2>(a, s);
-    return launch_tiles<uint16_t, DATA, 256, 256, 2, 4>(a, s);
+    return dtype == CBW_F32 ? launch_rows<float, DATA>(a, s) : launch_rows<uint16_t, DATA>(a, s);
 }
 
+// Weight gradient, bf16: large tiles where an expert's rows make the product
+// outweigh a tile's start and end (us, 256 x 256 | 128 x 128: 1024 rows for
+// each of 64 experts, 2048 -> 1408: 490 | 592; 512 on average: 323 | 338; 36
+// experts of 193, 1736 -> 1312: 205 | 190; 47 of 4, 816 -> 280: 22 | 17).
 hipError_t launch_expert_bwd_weight(int dtype, const ExpertArgs& a, hipStream_t s)
 {
-    hipError_t e = dtype == CBW_F32 ? launch_tiles<float, WEIGHT, 64, 64, 2, 2>(a, s)
-                                    : launch_tiles<uint16_t, WEIGHT, 256, 256, 2, 4>(a, s);
+    const int64_t mean = std::min<int64_t>(a.rows / std::max<int64_t>(1, std::min<int64_t>(a.E, a.rows)), a.split_rows);
+    const int64_t tiles = (int64_t)((a.C + 255) / 256) * ((a.K + 255) / 256) * (a.rows / a.split_rows + a.E);
+    hipError_t e;
+    if (dtype == CBW_F32) e = launch_tiles<float, WEIGHT, 64, 64, 2, 2>(a, s);
+    else if (mean >= 400 && tiles >= 256) e = launch_tiles<uint16_t, WEIGHT, 256, 256, 2, 4>(a, s);
+    else e = launch_tiles<uint16_t, WEIGHT, 128, 128, 2, 2>(a, s);
     if (e != hipSuccess || a.rows <= a.split_rows) return e;
-    expert_sum_kernel<<<2048, 256, 0, s>>>(a);
+    expert_sum_kernel<<<1024, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
