@@ -443,7 +443,8 @@ typedef struct {
 } cbw_norm_params;
 
 /* Host-only check.  CBW_ERR_UNSUPPORTED: C over 16384, C or a stride not a
- * multiple of 8, a bf16 stream beside a float32 block. */
+ * multiple of 8, a bf16 stream beside a float32 block, more than 2^31 - 1
+ * rows, a stride over 2^20 elements. */
 int cbw_validate_norm_desc(const cbw_norm_desc* desc);
 
 /* Workspace bytes of block_norm_bwd (host only). */

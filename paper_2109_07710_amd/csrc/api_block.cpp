@@ -97,13 +97,26 @@ NormRegions norm_regions(const cbw_norm_desc* d, const NormSplit& s)
 
 // ---------------------------------------------------------------- gradients
 
-int64_t grad_chunks(int64_t count) { return (count + kGradChunk - 1) / kGradChunk; }
+int64_t grad_bytes(const cbw_grad& g) { return g.count * (g.dtype == CBW_F32 ? 4 : 2); }
+int64_t grad_chunks(const cbw_grad& g) { return (grad_bytes(g) + kGradChunk - 1) / kGradChunk; }
 
-// Checks the list and counts its chunks.
-int check_grads(const cbw_grad* grads, int32_t n, bool with_out, int64_t* chunks)
+// What a call has to do: tensors with elements, and their chunks.
+struct GradWork {
+    int64_t tensors, chunks;
+    // the workspace: partial sums, one more for each launch after the first
+    // (rounding), then the table of all tensors
+    size_t partial_bytes() const
+    {
+        return ((size_t)(kGradMaxWgs + (tensors + kGradTable - 1) / kGradTable) * sizeof(double) + 255) & ~(size_t)255;
+    }
+    size_t ws_bytes() const { return partial_bytes() + (((size_t)tensors * sizeof(GradEntry) + 255) & ~(size_t)255); }
+};
+
+// Checks the list and sums up its work.
+int check_grads(const cbw_grad* grads, int32_t n, bool with_out, GradWork* work)
 {
     if (n < 0 || (n > 0 && !grads)) return CBW_ERR_INVALID_ARG;
-    *chunks = 0;
+    *work = {};
     for (int32_t i = 0; i < n; ++i) {
         const cbw_grad& g = grads[i];
         if (g.count < 0 || !known_dtype(g.dtype) || g.reserved != 0) return CBW_ERR_INVALID_ARG;
@@ -112,21 +125,11 @@ int check_grads(const cbw_grad* grads, int32_t n, bool with_out, int64_t* chunks
         const uintptr_t size = g.dtype == CBW_F32 ? 4 : 2;
         if (!aligned(g.grad, size) || (with_out && !aligned(g.out, size))) return CBW_ERR_UNSUPPORTED;
         if (g.count > ((int64_t)1 << 40)) return CBW_ERR_UNSUPPORTED;
-        *chunks += grad_chunks(g.count);
+        work->chunks += grad_chunks(g);
+        ++work->tensors;
+        if (work->chunks > 0x3fffffff) return CBW_ERR_UNSUPPORTED;
     }
-    return *chunks <= 0x3fffffff ? CBW_OK : CBW_ERR_UNSUPPORTED;
-}
-
-int64_t grad_launches(const cbw_grad* grads, int32_t n)
-{
-    int64_t k = 0;
-    for (int32_t i = 0; i < n; ++i) k += grads[i].count > 0;
-    return (k + kGradTable - 1) / kGradTable;
-}
-
-size_t grad_ws_bytes(const cbw_grad* grads, int32_t n)
-{
-    return round256((size_t)(kGradMaxWgs + grad_launches(grads, n)) * sizeof(double));
+    return CBW_OK;
 }
 
 // The next table of at most kGradTable tensors from entry `i` on; i moves on.
@@ -136,11 +139,8 @@ bool next_table(const cbw_grad* grads, int32_t n, int32_t& i, GradTable& t)
     for (; i < n && t.n < kGradTable; ++i) {
         const cbw_grad& g = grads[i];
         if (g.count == 0) continue;
-        t.src[t.n] = g.grad;
-        t.dst[t.n] = g.out;
-        t.count[t.n] = g.count | (g.dtype == CBW_BF16 ? INT64_MIN : 0);
-        t.first[t.n] = t.chunks;
-        t.chunks += (int32_t)grad_chunks(g.count);
+        t.e[t.n] = {g.grad, g.out, grad_bytes(g) | (g.dtype == CBW_BF16 ? INT64_MIN : 0), t.chunks, 0};
+        t.chunks += (int32_t)grad_chunks(g);
         ++t.n;
     }
     return t.n > 0;
@@ -152,29 +152,33 @@ int grad_grid(int64_t chunks, int64_t all)
     return (int)std::min(chunks, std::max<int64_t>(1, kGradMaxWgs * chunks / std::max<int64_t>(all, kGradMaxWgs)));
 }
 
-// Partials of all tensors into the workspace; their number.
-int norm_pass(const cbw_grad* grads, int32_t n, int32_t kind, int64_t chunks, double* partial, hipStream_t s, int* count)
+// Partials of all tensors into the workspace, with `table` the tensors as well; the number of partials.
+int norm_pass(const cbw_grad* grads, int32_t n, int32_t kind, const GradWork& work, double* partial, GradEntry* table,
+              hipStream_t s, int* count)
 {
     GradTable t;
+    t.entry0 = t.chunk0 = 0;
     *count = 0;
     for (int32_t i = 0; next_table(grads, n, i, t);) {
-        const int grid = grad_grid(t.chunks, chunks);
-        const hipError_t e = launch_grad_norm(t, kind, grid, partial + *count, s);
+        const int grid = grad_grid(t.chunks, work.chunks);
+        const hipError_t e = launch_grad_norm(t, kind, grid, partial + *count, table, s);
         if (e != hipSuccess) return hip_status(e);
         *count += grid;
+        t.entry0 += t.n;
+        t.chunk0 += t.chunks;
     }
     return CBW_OK;
 }
 
 int check_norm_call(const cbw_grad* grads, int32_t n, int32_t kind, bool with_out, const float* norm, const void* ws,
-                    size_t ws_bytes, int64_t* chunks)
+                    size_t ws_bytes, GradWork* work)
 {
-    int st = check_grads(grads, n, with_out, chunks);
+    int st = check_grads(grads, n, with_out, work);
     if (st != CBW_OK) return st;
     if (kind != CBW_GRAD_NORM_2 && kind != CBW_GRAD_NORM_INF) return CBW_ERR_INVALID_ARG;
     if (!norm) return CBW_ERR_INVALID_ARG;
     if (!aligned(norm, 4)) return CBW_ERR_UNSUPPORTED;
-    return check_ws(ws, ws_bytes, grad_ws_bytes(grads, n));
+    return check_ws(ws, ws_bytes, work->ws_bytes());
 }
 
 }  // namespace
@@ -258,7 +262,7 @@ int cbw_validate_norm_desc(const cbw_norm_desc* d)
     if (d->C > kNormMaxC || d->C % 8 || d->res_stride % 8 || d->block_stride % 8 || d->gate_stride % 8)
         return CBW_ERR_UNSUPPORTED;
     if (d->dtype == CBW_F32 && d->res_dtype != CBW_F32) return CBW_ERR_UNSUPPORTED;
-    if (d->rows > (int64_t)1 << 40 || d->res_stride > (int64_t)1 << 20 || d->block_stride > (int64_t)1 << 20 ||
+    if (d->rows > 0x7fffffff || d->res_stride > (int64_t)1 << 20 || d->block_stride > (int64_t)1 << 20 ||
         d->gate_stride > (int64_t)1 << 20)
         return CBW_ERR_UNSUPPORTED;
     return CBW_OK;
@@ -309,6 +313,7 @@ int block_norm_fwd(const cbw_norm_desc* desc, const void* x, const void* u, cons
     a.post = desc->post_norm;
     a.act = desc->gate_act;
     a.eps = desc->eps;
+    a.gate_div = make_fastdiv((uint32_t)std::min(desc->gate_rows, desc->rows));
     return hip_status(launch_norm_fwd(desc->dtype, desc->res_dtype, a, static_cast<hipStream_t>(stream)));
 }
 
@@ -372,46 +377,41 @@ int block_norm_bwd(const cbw_norm_desc* desc, const void* y, const void* u, cons
 int cbw_grad_workspace_size(const cbw_grad* grads, int32_t n, size_t* bytes)
 {
     if (!bytes) return CBW_ERR_INVALID_ARG;
-    int64_t chunks;
-    const int st = check_grads(grads, n, false, &chunks);
+    GradWork work;
+    const int st = check_grads(grads, n, false, &work);
     if (st != CBW_OK) return st;
-    *bytes = grad_ws_bytes(grads, n);
+    *bytes = work.ws_bytes();
     return CBW_OK;
 }
 
 int grad_norm(const cbw_grad* grads, int32_t n, int32_t kind, float* norm, void* workspace, size_t workspace_bytes,
               void* stream)
 {
-    int64_t chunks;
-    int st = check_norm_call(grads, n, kind, false, norm, workspace, workspace_bytes, &chunks);
+    GradWork work;
+    int st = check_norm_call(grads, n, kind, false, norm, workspace, workspace_bytes, &work);
     if (st != CBW_OK) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
     double* partial = static_cast<double*>(workspace);
     int count;
-    if ((st = norm_pass(grads, n, kind, chunks, partial, s, &count)) != CBW_OK) return st;
+    if ((st = norm_pass(grads, n, kind, work, partial, nullptr, s, &count)) != CBW_OK) return st;
     return hip_status(launch_grad_finish(kind, partial, count, norm, s));
 }
 
 int grad_clip(const cbw_grad* grads, int32_t n, int32_t kind, float max_norm, float* norm, void* workspace,
               size_t workspace_bytes, void* stream)
 {
-    int64_t chunks;
-    int st = check_norm_call(grads, n, kind, true, norm, workspace, workspace_bytes, &chunks);
+    GradWork work;
+    int st = check_norm_call(grads, n, kind, true, norm, workspace, workspace_bytes, &work);
     if (st != CBW_OK) return st;
     if (!(max_norm >= 0.f)) return CBW_ERR_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
     double* partial = static_cast<double*>(workspace);
+    GradEntry* table = reinterpret_cast<GradEntry*>(static_cast<char*>(workspace) + work.partial_bytes());
     int count;
-    if ((st = norm_pass(grads, n, kind, chunks, partial, s, &count)) != CBW_OK) return st;
-    GradTable t;
-    bool first = true;
-    for (int32_t i = 0; next_table(grads, n, i, t) || first; first = false) {
-        // (without tensors one workgroup writes the norm, 0, and c)
-        const int grid = t.n ? grad_grid(t.chunks, chunks) : 1;
-        const hipError_t e = launch_grad_scale(t, kind, grid, partial, count, max_norm, first ? norm : nullptr, s);
-        if (e != hipSuccess) return hip_status(e);
-    }
-    return CBW_OK;
+    if ((st = norm_pass(grads, n, kind, work, partial, table, s, &count)) != CBW_OK) return st;
+    // (without tensors one workgroup writes the norm, 0, and c)
+    const int grid = work.chunks ? grad_grid(work.chunks, work.chunks) : 1;
+    return hip_status(launch_grad_scale(table, (int)work.tensors, (int)work.chunks, kind, grid, partial, count, max_norm, norm, s));
 }
 
 }  // extern "C"

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "../../include/convbwd.h"
+#include "common.hpp"
 
 namespace cbw {
 
@@ -27,15 +28,15 @@ inline NormShape norm_shape(int C)
 {
     NormShape s;
     const int vecs = (C + 7) / 8;
-    if (vecs <= 128) {
+    if (vecs <= 64) {
         s.team = 8;
-        while (s.team < 64 && s.team < vecs) s.team *= 2;
-        s.vpt = vecs > s.team ? 2 : 1;
+        while (s.team < vecs) s.team *= 2;
+        s.vpt = 1;
         s.threads = 256;
         s.slots = s.threads / s.team;
     } else {
-        s.vpt = 2;
-        s.team = (vecs + 127) / 128 * 64;
+        s.vpt = vecs > 1024 ? 2 : 1;
+        s.team = (vecs + 64 * s.vpt - 1) / (64 * s.vpt) * 64;
         s.threads = s.team;
         s.slots = 1;
     }
@@ -63,6 +64,7 @@ struct NormArgs {
     int64_t rows, res_stride, block_stride, gate_stride, gate_rows;
     int C, pre, post, act;
     float eps;
+    FastDiv gate_div;           // by gate_rows
 };
 
 struct NormBackArgs {
@@ -113,22 +115,26 @@ hipError_t launch_expert_bwd_weight(int dtype, const ExpertArgs& a, hipStream_t 
 
 // ------------------------------------------------------- gradient clipping
 
-constexpr int kGradTable = 128;       // tensors per launch: the table travels in the kernel's arguments
-constexpr int kGradChunk = 8192;      // elements a workgroup takes at a time
+constexpr int kGradTable = 120;       // tensors per launch: the table travels in the kernel's arguments
+constexpr int kGradChunk = 16384;     // bytes a workgroup takes at a time
 constexpr int kGradMaxWgs = 1024;     // workgroups of all launches of a pass together, one more each for rounding
 
-struct GradTable {
-    const void* src[kGradTable];
-    void* dst[kGradTable];
-    int64_t count[kGradTable];        // bit 63: bf16
-    int32_t first[kGradTable];        // first chunk of the tensor in this launch
-    int32_t n, chunks;                // tensors and chunks of this launch
+struct GradEntry {
+    const void* src;
+    void* dst;
+    int64_t bytes;              // bit 63: bf16
+    int32_t first, pad;         // first chunk of the tensor
 };
-static_assert(sizeof(GradTable) <= 3840, "the table fits the kernel arguments");
+struct GradTable {
+    GradEntry e[kGradTable];
+    int32_t n, chunks;          // tensors and chunks of this launch
+    int32_t entry0, chunk0;     // of the launches before it
+};
+static_assert(sizeof(GradTable) <= 3872, "the table fits the kernel arguments");
 
-hipError_t launch_grad_norm(const GradTable& t, int kind, int grid, double* partial, hipStream_t s);
+hipError_t launch_grad_norm(const GradTable& t, int kind, int grid, double* partial, GradEntry* table, hipStream_t s);
 hipError_t launch_grad_finish(int kind, const double* partial, int npartial, float* norm, hipStream_t s);
-hipError_t launch_grad_scale(const GradTable& t, int kind, int grid, const double* partial, int npartial, float max_norm,
-                             float* norm, hipStream_t s);
+hipError_t launch_grad_scale(const GradEntry* table, int n, int chunks, int kind, int grid, const double* partial,
+                             int npartial, float max_norm, float* norm, hipStream_t s);
 
 }  // namespace cbw

@@ -19,6 +19,7 @@
 #include "block_kernels.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace cbw {
 namespace {
@@ -27,38 +28,89 @@ struct V8 {
     float f[8];
 };
 
-__device__ __forceinline__ V8 unpack(const uint4& a)
-{
-    V8 r;
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+// Eight consecutive elements as they lie in memory (16-byte aligned), kept
+// packed until their row's turn.
+template <typename T> struct Raw8;
+template <> struct Raw8<uint16_t> {
+    uint4 v;
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t off) { v = buf_load16(r, off); }
+    __device__ __forceinline__ V8 expand() const
+    {
+        V8 r;
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        r.f[2 * i] = __uint_as_float(w[i] << 16);
-        r.f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < 4; ++i) {
+            r.f[2 * i] = __uint_as_float(w[i] << 16);
+            r.f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+        return r;
     }
-    return r;
-}
-
-// Eight consecutive elements (16-byte aligned) as float32.
-__device__ __forceinline__ V8 load8(const uint16_t* p) { return unpack(*reinterpret_cast<const uint4*>(p)); }
-__device__ __forceinline__ V8 load8(const float* p)
+};
+template <> struct Raw8<float> {
+    uint4 a, b;
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t off)
+    {
+        a = buf_load16(r, off);
+        b = buf_load16(r, off + 16);
+    }
+    __device__ __forceinline__ V8 expand() const
+    {
+        return V8{{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                   __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)}};
+    }
+};
+__device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t r, uint32_t off, const V8& v, uint16_t)
 {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    return V8{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+    const u32x4 w = {pack_bf16x2(v.f[0], v.f[1]), pack_bf16x2(v.f[2], v.f[3]), pack_bf16x2(v.f[4], v.f[5]),
+                     pack_bf16x2(v.f[6], v.f[7])};
+    __builtin_amdgcn_raw_buffer_store_b128(w, r, off, 0, 0);
 }
-__device__ __forceinline__ void store8(uint16_t* p, const V8& v)
+__device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t r, uint32_t off, const V8& v, float)
 {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v.f[0], v.f[1]), pack_bf16x2(v.f[2], v.f[3]),
-                                              pack_bf16x2(v.f[4], v.f[5]), pack_bf16x2(v.f[6], v.f[7]));
-}
-__device__ __forceinline__ void store8(float* p, const V8& v)
-{
-    reinterpret_cast<float4*>(p)[0] = make_float4(v.f[0], v.f[1], v.f[2], v.f[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(v.f[4], v.f[5], v.f[6], v.f[7]);
+    const floatx4 a = {v.f[0], v.f[1], v.f[2], v.f[3]}, b = {v.f[4], v.f[5], v.f[6], v.f[7]};
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, a), r, off, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, b), r, off + 16, 0, 0);
 }
 __device__ __forceinline__ V8 splat(float v) { return V8{{v, v, v, v, v, v, v, v}}; }
 // A parameter's vector, or its neutral value where the caller has none.
-__device__ __forceinline__ V8 param8(const float* p, int c, float neutral) { return p ? load8(p + c) : splat(neutral); }
+__device__ __forceinline__ V8 param8(const float* p, int c, bool in, float neutral)
+{
+    if (!p || !in) return splat(neutral);
+    const float4 a = reinterpret_cast<const float4*>(p + c)[0], b = reinterpret_cast<const float4*>(p + c)[1];
+    return V8{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+}
+
+// Rows `row` and on of a tensor whose rows lie `stride` elements apart.  Lane
+// offsets are relative to that row; kOOB (a column or a row that does not
+// exist, or no tensor at all) reads zeros and writes nothing.
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const void* p, int64_t row, int64_t stride)
+{
+    return make_rsrc(static_cast<const T*>(p) + row * stride, p ? 0x7fffffffu : 0u);
+}
+
+// Sum over the 2^k lanes of a team: within groups of 4, 8 and 16 lanes by
+// register moves (the mirrors meet the other half), then by exchanging rows of
+// 16 and halves of the wave.  Every lane has the same result, bit for bit.
+__device__ __forceinline__ float lanes_sum(float v, int team)
+{
+    auto moved = [](float x, auto ctrl) {
+        return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, false));
+    };
+    v += moved(v, std::integral_constant<int, 0xb1>{});    // lane ^ 1
+    v += moved(v, std::integral_constant<int, 0x4e>{});    // lane ^ 2
+    v += moved(v, std::integral_constant<int, 0x141>{});   // mirrored in 8
+    if (team >= 16) v += moved(v, std::integral_constant<int, 0x140>{});   // mirrored in 16
+    if (team >= 32) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    if (team >= 64) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    return v;
+}
 
 // The threads that hold one row.  WIDE: a whole workgroup of `team` threads;
 // otherwise `team` lanes of a wave, several rows side by side.
@@ -76,28 +128,25 @@ struct Team {
     // Sums of two values over the team; every thread has them.  The halves of
     // the buffer alternate, so that a wave that is ahead by one sum does not
     // overwrite what another still reads: one barrier a sum.
-    __device__ void sum(float& a, float& b, float (*exch)[2][16])
+    __device__ void sum(float& a, float& b, float (*exch)[16][2])
     {
-        const int span = WIDE ? 64 : size;
-        for (int o = span / 2; o >= 1; o >>= 1) {
-            a += __shfl_xor(a, o);
-            b += __shfl_xor(b, o);
-        }
+        a = lanes_sum(a, WIDE ? 64 : size);
+        b = lanes_sum(b, WIDE ? 64 : size);
         if (!WIDE) return;
         const int wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0) {
-            exch[turn][0][wave] = a;
-            exch[turn][1][wave] = b;
+            exch[turn][wave][0] = a;
+            exch[turn][wave][1] = b;
         }
         __syncthreads();
         a = b = 0.f;
         for (int w = 0; w < size / 64; ++w) {
-            a += exch[turn][0][w];
-            b += exch[turn][1][w];
+            a += exch[turn][w][0];
+            b += exch[turn][w][1];
         }
         turn ^= 1;
     }
-    __device__ float sum(float a, float (*exch)[2][16])
+    __device__ float sum(float a, float (*exch)[16][2])
     {
         float b = 0.f;
         sum(a, b, exch);
@@ -114,7 +163,7 @@ __device__ __forceinline__ float gate_value(float g, int act)
 // Mean and reciprocal deviation of the row v (columns past C hold zeros).
 template <bool WIDE, int VPT>
 __device__ __forceinline__ void row_stats(Team<WIDE>& t, const V8 (&v)[VPT], const bool (&in)[VPT], int C, int kind, float eps,
-                                          float& mu, float& r, float (*exch)[2][16])
+                                          float& mu, float& r, float (*exch)[16][2])
 {
     mu = 0.f;
     if (kind == CBW_NORM_LAYER) {
@@ -138,12 +187,13 @@ __device__ __forceinline__ void row_stats(Team<WIDE>& t, const V8 (&v)[VPT], con
 
 // WT: 0 where a workgroup of 256 threads holds several rows, else one row to a
 // workgroup of up to WT threads (the bound lets the smaller ones keep more
-// registers).
+// registers).  The next rows' loads go out before a row is worked on, except
+// with more than 512 threads, whose registers cannot hold both.
 template <typename TR, typename TB, int WT, int VPT>
 __global__ __launch_bounds__(WT ? WT : 256) void norm_fwd_kernel(NormArgs a, int team)
 {
-    constexpr bool WIDE = WT != 0;
-    __shared__ float exch[2][2][16];
+    constexpr bool WIDE = WT != 0, AHEAD = WT != 1024;
+    __shared__ float exch[2][16][2];
     Team<WIDE> t(team);
     const int slots = WIDE ? 1 : 256 / team;
     bool in[VPT];
@@ -153,69 +203,97 @@ __global__ __launch_bounds__(WT ? WT : 256) void norm_fwd_kernel(NormArgs a, int
         col[i] = (i * team + t.lane) * 8;
         in[i] = col[i] < a.C;
     }
-    for (int64_t base = (int64_t)blockIdx.x * slots; base < a.rows; base += (int64_t)gridDim.x * slots) {
-        const int64_t row = base + t.slot;
-        const bool live = row < a.rows;
+    struct Loaded {
+        Raw8<TR> x[VPT];
+        Raw8<TB> u[VPT], g[VPT];
+    };
+    auto load = [&](Loaded& l, int64_t base) {
+        const bool live = base + t.slot < a.rows;
+        const auto rx = rows_at<TR>(a.x, base, a.res_stride);
+        const auto ru = rows_at<TB>(a.u, base, a.block_stride);
+        // (a row past the last one is not read, but its gate row must be a number)
+        const uint32_t g0 = fdiv((uint32_t)min(base, a.rows - 1), a.gate_div);
+        const uint32_t dg = fdiv((uint32_t)min(base + t.slot, a.rows - 1), a.gate_div) - g0;
+        const auto rg = rows_at<TB>(a.gate, g0, a.gate_stride);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const uint32_t dead = live && in[i] ? 0u : kOOB;
+            l.x[i].load(rx, (uint32_t)(t.slot * a.res_stride + col[i]) * (uint32_t)sizeof(TR) | dead);
+            l.u[i].load(ru, (uint32_t)(t.slot * a.block_stride + col[i]) * (uint32_t)sizeof(TB) | dead);
+            l.g[i].load(rg, (uint32_t)(dg * a.gate_stride + col[i]) * (uint32_t)sizeof(TB) | dead);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * slots;
+    Loaded next;
+    if (AHEAD) load(next, (int64_t)blockIdx.x * slots);
+    for (int64_t base = (int64_t)blockIdx.x * slots; base < a.rows; base += step) {
+        if (!AHEAD) load(next, base);
+        const bool live = base + t.slot < a.rows;
         V8 y[VPT], u[VPT], g[VPT];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const bool ok = live && in[i];
-            y[i] = ok ? load8(static_cast<const TR*>(a.x) + row * a.res_stride + col[i]) : splat(0.f);
-            u[i] = ok && a.u ? load8(static_cast<const TB*>(a.u) + row * a.block_stride + col[i]) : splat(0.f);
-            g[i] = ok && a.gate ? load8(static_cast<const TB*>(a.gate) +
-                                        (a.gate_rows > 1 ? row / a.gate_rows : row) * a.gate_stride + col[i])
-                                : splat(0.f);
+            y[i] = next.x[i].expand();
+            u[i] = next.u[i].expand();
+            g[i] = next.g[i].expand();
         }
+        if (AHEAD && base + step < a.rows) load(next, base + step);
         float mu_u = 0.f, r_u = 0.f, mu_y = 0.f, r_y = 0.f;
         if (a.u) {
             if (a.post != CBW_NORM_NONE) row_stats<WIDE, VPT>(t, u, in, a.C, a.post, a.eps, mu_u, r_u, exch);
+            const auto ry = rows_at<TR>(a.y, base, a.res_stride);
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                if (!in[i]) continue;
-                const V8 w = param8(a.w_post, col[i], 1.f), b = param8(a.b_post, col[i], 0.f),
-                         s = param8(a.scale, col[i], 1.f);
+                const V8 w = param8(a.w_post, col[i], in[i], 1.f), b = param8(a.b_post, col[i], in[i], 0.f),
+                         s = param8(a.scale, col[i], in[i], 1.f);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float n = a.post == CBW_NORM_NONE ? u[i].f[j] : (u[i].f[j] - mu_u) * r_u;
+                    // (columns past C stay zeros)
+                    const float n = a.post == CBW_NORM_NONE ? u[i].f[j] : in[i] ? (u[i].f[j] - mu_u) * r_u : 0.f;
                     const float z = fmaf(n, w.f[j], b.f[j]) * s.f[j];
                     y[i].f[j] = fmaf(z, a.gate ? gate_value(g[i].f[j], a.act) : 1.f, y[i].f[j]);
                 }
-                if (live) store8(static_cast<TR*>(a.y) + row * a.res_stride + col[i], y[i]);
+                store8(ry, (uint32_t)(t.slot * a.res_stride + col[i]) * (uint32_t)sizeof(TR) | (live && in[i] ? 0u : kOOB), y[i],
+                       TR{});
             }
         }
         if (a.h) {
             row_stats<WIDE, VPT>(t, y, in, a.C, a.pre, a.eps, mu_y, r_y, exch);
+            const auto rh = rows_at<TB>(a.h, base, a.block_stride);
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                if (!in[i]) continue;
-                const V8 w = param8(a.w_pre, col[i], 1.f), b = param8(a.b_pre, col[i], 0.f);
+                const V8 w = param8(a.w_pre, col[i], in[i], 1.f), b = param8(a.b_pre, col[i], in[i], 0.f);
                 V8 h;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) h.f[j] = fmaf((y[i].f[j] - mu_y) * r_y, w.f[j], b.f[j]);
-                if (live) store8(static_cast<TB*>(a.h) + row * a.block_stride + col[i], h);
+                store8(rh, (uint32_t)(t.slot * a.block_stride + col[i]) * (uint32_t)sizeof(TB) | (live && in[i] ? 0u : kOOB), h,
+                       TB{});
             }
         }
         if (a.stats && live && t.lane == 0)
-            reinterpret_cast<float4*>(a.stats)[row] = make_float4(mu_y, r_y, mu_u, r_u);
+            reinterpret_cast<float4*>(a.stats)[base + t.slot] = make_float4(mu_y, r_y, mu_u, r_u);
     }
 }
 
 // FULL: gradients of biases or the scale are asked for as well (their sums
 // take registers that the usual call has no use for).
 template <typename TR, typename TB, int WT, int VPT, bool FULL>
-__global__ __launch_bounds__(WT ? WT : 256) void norm_bwd_kernel(NormBackArgs a, int team)
+__global__ __launch_bounds__(WT ? WT : 256, WT == 512 && !FULL && sizeof(TB) == 2 ? 4 : 1) void norm_bwd_kernel(NormBackArgs a, int team)
 {
-    constexpr bool WIDE = WT != 0;
-    __shared__ float exch[2][2][16];
+    constexpr bool WIDE = WT != 0, AHEAD = WT != 1024;
+    __shared__ float exch[2][16][2];
     __shared__ float comb_s[WIDE ? 1 : 256 * 8];
     Team<WIDE> t(team);
     const int slots = WIDE ? 1 : 256 / team;
     bool in[VPT];
     int col[VPT];
+    uint32_t res_off[VPT], blk_off[VPT];   // byte offsets from a workgroup's first row, kOOB past the last column
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         col[i] = (i * team + t.lane) * 8;
         in[i] = col[i] < a.C;
+        const uint32_t dead = in[i] ? 0u : kOOB;
+        res_off[i] = (uint32_t)(t.slot * a.res_stride + col[i]) * (uint32_t)sizeof(TR) | dead;
+        blk_off[i] = (uint32_t)(t.slot * a.block_stride + col[i]) * (uint32_t)sizeof(TB) | dead;
     }
     V8 acc[NG_COUNT][VPT];   // (without FULL all but two stay zeros and take no registers)
 #pragma unroll
@@ -238,47 +316,83 @@ __global__ __launch_bounds__(WT ? WT : 256) void norm_bwd_kernel(NormBackArgs a,
                 for (int j = 0; j < 8; ++j) v.f[j] += comb_s[j * 256 + s * team + t.lane];
     };
 
+    // Parameters: of narrow rows, which pass quickly, kept in registers; of
+    // wide ones read at every row (they are in the L1 or L2, and the registers
+    // hold another wave instead).
+    struct Params {
+        V8 w_pre, w_post, b_post, scale;
+    };
+    auto params_at = [&](int i) {
+        return Params{param8(a.w_pre, col[i], in[i], 1.f), param8(a.w_post, col[i], in[i], 1.f),
+                      param8(a.b_post, col[i], in[i], 0.f), param8(a.scale, col[i], in[i], 1.f)};
+    };
+    Params kept[WIDE ? 1 : VPT];
+    if (!WIDE)
+#pragma unroll
+        for (int i = 0; i < (WIDE ? 1 : VPT); ++i) kept[i] = params_at(i);
+
+    struct Loaded {
+        Raw8<TR> y[VPT], dy[VPT];
+        Raw8<TB> dh[VPT], u[VPT], g[VPT];
+        uint4 st;
+    };
     const int64_t i0 = blockIdx.x * a.split.items / gridDim.x, i1 = (blockIdx.x + 1) * a.split.items / gridDim.x;
     for (int64_t item = i0; item < i1; ++item) {
         const int64_t group = item / a.split.parts, part = item - group * a.split.parts;
         const int64_t g0 = group * a.split.group_rows, g1 = min(g0 + a.split.group_rows, a.rows);
         const int64_t r0 = min(g0 + part * a.split.item_rows, g1), r1 = min(r0 + a.split.item_rows, g1);
+        auto load = [&](Loaded& l, int64_t base) {
+            const auto ry = rows_at<TR>(a.dh ? a.y : nullptr, base, a.res_stride), rdy = rows_at<TR>(a.dy, base, a.res_stride);
+            const auto rdh = rows_at<TB>(a.dh, base, a.block_stride), ru = rows_at<TB>(a.u, base, a.block_stride);
+            const auto rg = rows_at<TB>(a.gate, a.gate_rows > 1 ? group : base, a.gate_stride);
+            const uint32_t dead = base + t.slot < r1 ? 0u : kOOB;
+            l.st = buf_load16(rows_at<float>(a.stats, base, 4), (uint32_t)t.slot * 16u | dead);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                l.y[i].load(ry, res_off[i] | dead);
+                l.dh[i].load(rdh, blk_off[i] | dead);
+                l.dy[i].load(rdy, res_off[i] | dead);
+                l.u[i].load(ru, blk_off[i] | dead);
+                l.g[i].load(rg, (uint32_t)((a.gate_rows > 1 ? 0 : t.slot) * a.gate_stride + col[i]) * (uint32_t)sizeof(TB) |
+                                    (in[i] ? dead : kOOB));
+            }
+        };
         V8 dgs[VPT];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) dgs[i] = splat(0.f);
+        Loaded next;
+        if (AHEAD && r0 < r1) load(next, r0);
         for (int64_t base = r0; base < r1; base += slots) {
-            const int64_t row = base + t.slot;
-            const bool live = row < r1;
-            V8 y[VPT], dh[VPT], dy[VPT], u[VPT], g[VPT];
-            float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (live) st = reinterpret_cast<const float4*>(a.stats)[row];
+            if (!AHEAD) load(next, base);
+            const uint32_t dead = base + t.slot < r1 ? 0u : kOOB;
+            V8 n[VPT], d[VPT], gy[VPT], u[VPT], g[VPT];
+            const float4 st = make_float4(__uint_as_float(next.st.x), __uint_as_float(next.st.y), __uint_as_float(next.st.z),
+                                          __uint_as_float(next.st.w));
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                const bool ok = live && in[i];
-                dy[i] = ok && a.dy ? load8(static_cast<const TR*>(a.dy) + row * a.res_stride + col[i]) : splat(0.f);
-                y[i] = ok && a.dh ? load8(static_cast<const TR*>(a.y) + row * a.res_stride + col[i]) : splat(0.f);
-                dh[i] = ok && a.dh ? load8(static_cast<const TB*>(a.dh) + row * a.block_stride + col[i]) : splat(0.f);
-                u[i] = ok && a.u ? load8(static_cast<const TB*>(a.u) + row * a.block_stride + col[i]) : splat(0.f);
-                g[i] = ok && a.gate ? load8(static_cast<const TB*>(a.gate) +
-                                            (a.gate_rows > 1 ? row / a.gate_rows : row) * a.gate_stride + col[i])
-                                    : splat(0.f);
+                n[i] = next.y[i].expand();
+                d[i] = next.dh[i].expand();
+                gy[i] = next.dy[i].expand();
+                u[i] = next.u[i].expand();
+                g[i] = next.g[i].expand();
             }
+            if (AHEAD && base + slots < r1) load(next, base + slots);
             if (a.dh) {
                 float sd = 0.f, sn = 0.f;
 #pragma unroll
                 for (int i = 0; i < VPT; ++i) {
-                    if (!in[i]) continue;
-                    const V8 w = param8(a.w_pre, col[i], 1.f);
+                    const V8 w = WIDE ? param8(a.w_pre, col[i], in[i], 1.f) : kept[WIDE ? 0 : i].w_pre;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float n = live ? (y[i].f[j] - st.x) * st.y : 0.f;
-                        acc[NG_W_PRE][i].f[j] = fmaf(dh[i].f[j], n, acc[NG_W_PRE][i].f[j]);
-                        if (FULL) acc[NG_B_PRE][i].f[j] += dh[i].f[j];
-                        const float d = dh[i].f[j] * w.f[j];
-                        y[i].f[j] = n;
-                        dh[i].f[j] = d;
-                        sd += d;
-                        sn = fmaf(d, n, sn);
+                        // (a row or column that does not exist: all loads and r are zero)
+                        const float v = in[i] ? (n[i].f[j] - st.x) * st.y : 0.f;
+                        acc[NG_W_PRE][i].f[j] = fmaf(d[i].f[j], v, acc[NG_W_PRE][i].f[j]);
+                        if (FULL) acc[NG_B_PRE][i].f[j] += d[i].f[j];
+                        const float e = d[i].f[j] * w.f[j];
+                        n[i].f[j] = v;
+                        d[i].f[j] = e;
+                        sd += e;
+                        sn = fmaf(e, v, sn);
                     }
                 }
                 t.sum(sd, sn, exch);
@@ -287,44 +401,41 @@ __global__ __launch_bounds__(WT ? WT : 256) void norm_bwd_kernel(NormBackArgs a,
                 for (int i = 0; i < VPT; ++i)
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        dy[i].f[j] = fmaf(st.y, dh[i].f[j] - md - y[i].f[j] * mn, dy[i].f[j]);
+                        gy[i].f[j] = in[i] ? fmaf(st.y, d[i].f[j] - md - n[i].f[j] * mn, gy[i].f[j]) : 0.f;
             }
+            const auto rdx = rows_at<TR>(a.dx, base, a.res_stride);
 #pragma unroll
-            for (int i = 0; i < VPT; ++i)
-                if (live && in[i]) store8(static_cast<TR*>(a.dx) + row * a.res_stride + col[i], dy[i]);
+            for (int i = 0; i < VPT; ++i) store8(rdx, res_off[i] | dead, gy[i], TR{});
             if (!a.u) continue;
             float sd = 0.f, sn = 0.f;
+            const auto rdg = rows_at<TB>(shared_gate ? nullptr : a.dgate, base, a.gate_stride);
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                if (!in[i]) continue;
-                const V8 w = param8(a.w_post, col[i], 1.f), b = param8(a.b_post, col[i], 0.f),
-                         s = param8(a.scale, col[i], 1.f);
+                const Params pm = WIDE ? params_at(i) : kept[WIDE ? 0 : i];
+                const V8 &w = pm.w_post, &b = pm.b_post, &s = pm.scale;
                 V8 dg;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float gy = live ? dy[i].f[j] : 0.f;
-                    const float n = a.post == CBW_NORM_NONE ? u[i].f[j] : live ? (u[i].f[j] - st.z) * st.w : 0.f;
-                    const float z = fmaf(n, w.f[j], b.f[j]);
+                    const float v = a.post == CBW_NORM_NONE ? u[i].f[j] : in[i] ? (u[i].f[j] - st.z) * st.w : 0.f;
+                    const float z = fmaf(v, w.f[j], b.f[j]);
                     const float act = a.gate ? gate_value(g[i].f[j], a.act) : 1.f;
                     const float da = a.act == CBW_GATE_SIGMOID ? act * (1.f - act) : 1.f;
-                    dg.f[j] = gy * s.f[j] * z * da;
-                    if (FULL) acc[NG_SCALE][i].f[j] = fmaf(gy * act, z, acc[NG_SCALE][i].f[j]);
-                    const float dz = gy * s.f[j] * act;
-                    acc[NG_W_POST][i].f[j] = fmaf(dz, n, acc[NG_W_POST][i].f[j]);
+                    dg.f[j] = gy[i].f[j] * s.f[j] * z * da;
+                    if (FULL) acc[NG_SCALE][i].f[j] = fmaf(gy[i].f[j] * act, z, acc[NG_SCALE][i].f[j]);
+                    const float dz = gy[i].f[j] * s.f[j] * act;
+                    acc[NG_W_POST][i].f[j] = fmaf(dz, v, acc[NG_W_POST][i].f[j]);
                     if (FULL) acc[NG_B_POST][i].f[j] += dz;
-                    const float d = dz * w.f[j];
-                    u[i].f[j] = n;
-                    g[i].f[j] = d;
-                    sd += d;
-                    sn = fmaf(d, n, sn);
+                    const float e = dz * w.f[j];
+                    u[i].f[j] = v;
+                    g[i].f[j] = e;
+                    sd += e;
+                    sn = fmaf(e, v, sn);
                 }
-                if (a.dgate) {
-                    if (shared_gate) {
+                if (shared_gate) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) dgs[i].f[j] += dg.f[j];
-                    } else if (live) {
-                        store8(static_cast<TB*>(a.dgate) + row * a.gate_stride + col[i], dg);
-                    }
+                    for (int j = 0; j < 8; ++j) dgs[i].f[j] += dg.f[j];
+                } else {
+                    store8(rdg, (uint32_t)(t.slot * a.gate_stride + col[i]) * (uint32_t)sizeof(TB) | (in[i] ? dead : kOOB), dg, TB{});
                 }
             }
             if (!a.du) continue;
@@ -336,17 +447,20 @@ __global__ __launch_bounds__(WT ? WT : 256) void norm_bwd_kernel(NormBackArgs a,
 #pragma unroll
                     for (int j = 0; j < 8; ++j) g[i].f[j] = st.w * (g[i].f[j] - md - u[i].f[j] * mn);
             }
+            const auto rdu = rows_at<TB>(a.du, base, a.block_stride);
 #pragma unroll
-            for (int i = 0; i < VPT; ++i)
-                if (live && in[i]) store8(static_cast<TB*>(a.du) + row * a.block_stride + col[i], g[i]);
+            for (int i = 0; i < VPT; ++i) store8(rdu, blk_off[i] | dead, g[i], TB{});
         }
         if (shared_gate) {
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
                 over_slots(dgs[i]);
-                if (t.slot != 0 || !in[i]) continue;
-                if (a.gate_partial) store8(a.gate_partial + item * a.C + col[i], dgs[i]);
-                else store8(static_cast<TB*>(a.dgate) + group * a.gate_stride + col[i], dgs[i]);
+                const bool mine = t.slot == 0 && in[i];
+                if (a.gate_partial)
+                    store8(rows_at<float>(a.gate_partial, item, a.C), mine ? (uint32_t)col[i] * 4u : kOOB, dgs[i], 0.f);
+                else
+                    store8(rows_at<TB>(a.dgate, group, a.gate_stride), mine ? (uint32_t)col[i] * (uint32_t)sizeof(TB) : kOOB,
+                           dgs[i], TB{});
             }
         }
     }
@@ -358,9 +472,8 @@ __global__ __launch_bounds__(WT ? WT : 256) void norm_bwd_kernel(NormBackArgs a,
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             over_slots(acc[k][i]);
-            if (t.slot != 0 || !in[i]) continue;
-            float* to = a.partial ? a.partial + (int64_t)blockIdx.x * a.C * NG_COUNT + at * a.C : a.grads[k];
-            store8(to + col[i], acc[k][i]);
+            const float* to = a.partial ? a.partial + (int64_t)blockIdx.x * a.C * NG_COUNT + at * a.C : a.grads[k];
+            store8(rows_at<float>(to, 0, 0), t.slot == 0 && in[i] ? (uint32_t)col[i] * 4u : kOOB, acc[k][i], 0.f);
         }
         ++at;
     }
@@ -399,16 +512,14 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(SumArgs a)
     const int64_t step = gate ? a.C : (int64_t)NG_COUNT * a.C, n = gate ? a.parts : a.n;
     float s = 0.f;
     if (c < a.C) {
-        int64_t i = wave;
-        for (; i + 48 < n; i += 64) {
-            const float v0 = p[i * step + c], v1 = p[(i + 16) * step + c], v2 = p[(i + 32) * step + c],
-                        v3 = p[(i + 48) * step + c];
-            s += v0;
-            s += v1;
-            s += v2;
-            s += v3;
+        // sixteen loads in flight, added in order
+        for (int64_t i = wave; i < n; i += 256) {
+            float v[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = i + 16 * k < n ? p[(i + 16 * k) * step + c] : 0.f;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) s += v[k];
         }
-        for (; i < n; i += 16) s += p[i * step + c];
     }
     sum_s[wave][lane] = s;
     __syncthreads();
@@ -423,16 +534,12 @@ hipError_t fwd_types(const NormArgs& a, hipStream_t s)
 {
     const NormShape n = norm_shape(a.C);
     const int64_t want = (a.rows + n.slots - 1) / n.slots;
-    const int grid = (int)std::min<int64_t>(want, 1 << 20);
-    if (n.slots == 1) {
-        if (n.team <= 256) norm_fwd_kernel<TR, TB, 256, 2><<<grid, n.threads, 0, s>>>(a, n.team);
-        else if (n.team <= 512) norm_fwd_kernel<TR, TB, 512, 2><<<grid, n.threads, 0, s>>>(a, n.team);
-        else norm_fwd_kernel<TR, TB, 1024, 2><<<grid, n.threads, 0, s>>>(a, n.team);
-    } else if (n.vpt == 1) {
-        norm_fwd_kernel<TR, TB, 0, 1><<<grid, n.threads, 0, s>>>(a, n.team);
-    } else {
-        norm_fwd_kernel<TR, TB, 0, 2><<<grid, n.threads, 0, s>>>(a, n.team);
-    }
+    // four workgroups of 256 threads a CU, each with rows enough to load ahead
+    const int grid = (int)std::min<int64_t>(want, 256 * std::max(1, 1024 / n.threads));
+    if (n.slots > 1) norm_fwd_kernel<TR, TB, 0, 1><<<grid, n.threads, 0, s>>>(a, n.team);
+    else if (n.vpt == 2) norm_fwd_kernel<TR, TB, 1024, 2><<<grid, n.threads, 0, s>>>(a, n.team);
+    else if (n.team <= 512) norm_fwd_kernel<TR, TB, 512, 1><<<grid, n.threads, 0, s>>>(a, n.team);
+    else norm_fwd_kernel<TR, TB, 1024, 1><<<grid, n.threads, 0, s>>>(a, n.team);
     return hipGetLastError();
 }
 
@@ -440,15 +547,11 @@ template <typename TR, typename TB, bool FULL>
 void bwd_shapes(const NormBackArgs& a, hipStream_t s)
 {
     const NormShape n = norm_shape(a.C);
-    if (n.slots == 1) {
-        if (n.team <= 256) norm_bwd_kernel<TR, TB, 256, 2, FULL><<<a.split.grid, n.threads, 0, s>>>(a, n.team);
-        else if (n.team <= 512) norm_bwd_kernel<TR, TB, 512, 2, FULL><<<a.split.grid, n.threads, 0, s>>>(a, n.team);
-        else norm_bwd_kernel<TR, TB, 1024, 2, FULL><<<a.split.grid, n.threads, 0, s>>>(a, n.team);
-    } else if (n.vpt == 1) {
-        norm_bwd_kernel<TR, TB, 0, 1, FULL><<<a.split.grid, n.threads, 0, s>>>(a, n.team);
-    } else {
-        norm_bwd_kernel<TR, TB, 0, 2, FULL><<<a.split.grid, n.threads, 0, s>>>(a, n.team);
-    }
+    const int grid = a.split.grid;
+    if (n.slots > 1) norm_bwd_kernel<TR, TB, 0, 1, FULL><<<grid, n.threads, 0, s>>>(a, n.team);
+    else if (n.vpt == 2) norm_bwd_kernel<TR, TB, 1024, 2, FULL><<<grid, n.threads, 0, s>>>(a, n.team);
+    else if (n.team <= 512) norm_bwd_kernel<TR, TB, 512, 1, FULL><<<grid, n.threads, 0, s>>>(a, n.team);
+    else norm_bwd_kernel<TR, TB, 1024, 1, FULL><<<grid, n.threads, 0, s>>>(a, n.team);
 }
 
 template <typename TR, typename TB>

@@ -4,12 +4,14 @@
 //   c = min(1, max_norm / (norm + 1e-6)),  out = c g
 //
 // Bound by memory: every gradient is read once for the norm and once more to
-// be scaled.  The tensors' addresses travel in the kernel arguments, 128 to a
+// be scaled.  The tensors' addresses travel in the kernel arguments, 120 to a
 // launch, so nothing is copied to the device and a captured call replays as
-// it was.  Each workgroup sums a contiguous range of chunks in a fixed order
-// and leaves one partial; the scaling kernel's workgroups each add all
-// partials in the same order (8 KB from the L2) instead of waiting for a
-// launch in between, so a call is two launches per 128 tensors.
+// it was; the norm's launches leave them in the workspace, where one scaling
+// launch finds all of them.  Each workgroup sums a contiguous range of chunks
+// in a fixed order and leaves one partial; the scaling kernel's workgroups
+// each add all partials in the same order (8 KB from the L2, under their
+// first chunk's loads) instead of waiting for a launch in between.  A call is
+// two launches, one more for every 120 tensors past the first.
 #include "common.hpp"
 #include "block_kernels.hpp"
 
@@ -62,18 +64,35 @@ __device__ double join_workgroup(R r)
     return all.value();
 }
 
-// The tensor that chunk `c` belongs to: the last one that starts at or before
-// it (tensors without elements start where the next one does).
-__device__ __forceinline__ int tensor_of(const GradTable& t, int c)
-{
-    int lo = 0, hi = t.n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (t.first[mid] <= c) lo = mid;
-        else hi = mid;
+// A workgroup's 16 KB of one tensor: four vectors a thread, and one of the up
+// to seven elements that are left past a tensor's last whole vector.
+struct Chunk {
+    static constexpr int U = kGradChunk / (16 * GT);
+    u32x4 v[U];
+    uint32_t left;      // the element's bits (bf16: its 16)
+    char* dst;
+    int n;              // bytes
+    bool bf16, has_left;
+
+    __device__ __forceinline__ int at(int i) const { return (i * GT + (int)threadIdx.x) * 16; }
+    __device__ __forceinline__ int left_at() const { return (n & ~15) + (int)threadIdx.x * (bf16 ? 2 : 4); }
+
+    __device__ __forceinline__ void load(const GradEntry& e, int c)
+    {
+        const int64_t b0 = (int64_t)(c - e.first) * kGradChunk, all = e.bytes & INT64_MAX;
+        const char* src = static_cast<const char*>(e.src) + b0;
+        dst = static_cast<char*>(e.dst) + b0;
+        n = (int)(all - b0 < kGradChunk ? all - b0 : kGradChunk);
+        bf16 = e.bytes < 0;
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            v[i] = at(i) + 16 <= n ? *reinterpret_cast<const u32x4_any*>(src + at(i)) : u32x4{0, 0, 0, 0};
+        has_left = left_at() < n;
+        left = 0;
+        if (has_left)
+            left = bf16 ? *reinterpret_cast<const uint16_t*>(src + left_at()) : *reinterpret_cast<const uint32_t*>(src + left_at());
     }
-    return lo;
-}
+};
 
 struct ChunkRange {
     int begin, end;
@@ -85,48 +104,46 @@ __device__ __forceinline__ ChunkRange my_chunks(int chunks)
 }
 
 template <typename R>
-__global__ __launch_bounds__(GT) void grad_norm_kernel(GradTable t, double* partial)
+__global__ __launch_bounds__(GT) void grad_norm_kernel(GradTable t, double* partial, GradEntry* table)
 {
-    R r;
+    const int lane = threadIdx.x & 63;
     const ChunkRange range = my_chunks(t.chunks);
+    // the tensor of the first chunk: the last one that starts at or before it
+    // (one look at all starts: a search would wait for the arguments, which
+    // lie far away, at every step)
+    const int f0 = lane < t.n ? t.e[lane].first : INT32_MAX;
+    const int f1 = lane + 64 < t.n ? t.e[lane + 64].first : INT32_MAX;
+    int k = __popcll(__ballot(f0 <= range.begin)) + __popcll(__ballot(f1 <= range.begin)) - 1;
+    static_assert(kGradTable <= 128, "two lookups a lane");
+    if (table && blockIdx.x == 0 && (int)threadIdx.x < t.n) {
+        GradEntry e = t.e[threadIdx.x];
+        e.first += t.chunk0;
+        table[t.entry0 + threadIdx.x] = e;
+    }
+    R r;
+    Chunk next;
+    next.load(t.e[k], range.begin);
     for (int c = range.begin; c < range.end; ++c) {
-        const int k = __builtin_amdgcn_readfirstlane(tensor_of(t, c));
-        const int64_t count = t.count[k] & 0x7fffffffffffffffll;
-        const int64_t e0 = (int64_t)(c - t.first[k]) * kGradChunk;
-        const int n = (int)(count - e0 < kGradChunk ? count - e0 : kGradChunk);
-        if (t.count[k] < 0) {
-            const uint16_t* src = static_cast<const uint16_t*>(t.src[k]) + e0;
-            constexpr int U = kGradChunk / (8 * GT);
-            u32x4 v[U];
+        const Chunk now = next;
+        if (c + 1 < range.end) {
+            if (k + 1 < t.n && t.e[k + 1].first <= c + 1) ++k;
+            next.load(t.e[k], c + 1);
+        }
+        if (now.bf16) {
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int e = (i * GT + (int)threadIdx.x) * 8;
-                v[i] = e + 8 <= n ? *reinterpret_cast<const u32x4_any*>(src + e) : u32x4{0, 0, 0, 0};
-            }
-#pragma unroll
-            for (int i = 0; i < U; ++i)
+            for (int i = 0; i < Chunk::U; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    r.add(bf16_lo(v[i][j]));
-                    r.add(bf16_hi(v[i][j]));
+                    r.add(bf16_lo(now.v[i][j]));
+                    r.add(bf16_hi(now.v[i][j]));
                 }
-            const int e = (n & ~7) + (int)threadIdx.x;
-            if (e < n) r.add(bf16_lo(src[e]));
+            r.add(bf16_lo(now.left));
         } else {
-            const float* src = static_cast<const float*>(t.src[k]) + e0;
-            constexpr int U = kGradChunk / (4 * GT);
-            u32x4 v[U];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int e = (i * GT + (int)threadIdx.x) * 4;
-                v[i] = e + 4 <= n ? *reinterpret_cast<const u32x4_any*>(src + e) : u32x4{0, 0, 0, 0};
-            }
+            for (int i = 0; i < Chunk::U; ++i)
 #pragma unroll
-            for (int i = 0; i < U; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) r.add(__uint_as_float(v[i][j]));
-            const int e = (n & ~3) + (int)threadIdx.x;
-            if (e < n) r.add(src[e]);
+                for (int j = 0; j < 4; ++j) r.add(__uint_as_float(now.v[i][j]));
+            r.add(__uint_as_float(now.left));
         }
     }
     const double sum = join_workgroup(r);
@@ -148,76 +165,70 @@ __global__ __launch_bounds__(GT) void grad_finish_kernel(const double* partial, 
     if (threadIdx.x == 0) norm[0] = (float)v;
 }
 
+// The tensor of chunk c in the table: a wave looks at 64 starts at a time.
+__device__ __forceinline__ int tensor_of(const GradEntry* table, int n, int c)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = n;   // the tensor lies in [lo, hi)
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+        lo += (__popcll(__ballot(i < hi && table[i < hi ? i : lo].first <= c)) - 1) * step;
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+
 // The chunks go backwards: those that the norm pass read last are the ones
 // that the 256 MB cache still holds.
 template <typename R>
-__global__ __launch_bounds__(GT) void grad_scale_kernel(GradTable t, const double* partial, int npartial, float max_norm,
-                                                        float* norm)
+__global__ __launch_bounds__(GT) void grad_scale_kernel(const GradEntry* table, int n, int chunks, const double* partial,
+                                                        int npartial, float max_norm, float* norm)
 {
+    const ChunkRange range = my_chunks(chunks);
+    int k = 0;
+    Chunk next;
+    if (chunks > 0) {
+        k = __builtin_amdgcn_readfirstlane(tensor_of(table, n, range.end - 1));
+        next.load(table[k], range.end - 1);
+    }
     const double total = norm_of<R>(partial, npartial);
     const double q = (double)max_norm / (total + 1e-6);
     const float coef = q >= 1.0 ? 1.0f : (float)q;   // (a NaN stays one)
-    if (norm && blockIdx.x == 0 && threadIdx.x == 0) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
         norm[0] = (float)total;
         norm[1] = coef;
     }
-    const ChunkRange range = my_chunks(t.chunks);
     for (int c = range.end - 1; c >= range.begin; --c) {
-        const int k = __builtin_amdgcn_readfirstlane(tensor_of(t, c));
-        const int64_t count = t.count[k] & 0x7fffffffffffffffll;
-        const int64_t e0 = (int64_t)(c - t.first[k]) * kGradChunk;
-        const int n = (int)(count - e0 < kGradChunk ? count - e0 : kGradChunk);
-        if (coef == 1.0f && t.src[k] == t.dst[k]) continue;   // in place and unclipped: every value stays
-        if (t.count[k] < 0) {
-            const uint16_t* src = static_cast<const uint16_t*>(t.src[k]) + e0;
-            uint16_t* dst = static_cast<uint16_t*>(t.dst[k]) + e0;
-            constexpr int U = kGradChunk / (8 * GT);
-            u32x4 v[U];
+        const Chunk now = next;
+        // in place and unclipped every value stays
+        const bool stays = coef == 1.0f && table[k].src == table[k].dst;
+        if (c > range.begin) {
+            if (table[k].first == c) --k;
+            if (!(coef == 1.0f && table[k].src == table[k].dst)) next.load(table[k], c - 1);
+        }
+        if (stays) continue;
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int e = (i * GT + (int)threadIdx.x) * 8;
-                v[i] = e + 8 <= n ? *reinterpret_cast<const u32x4_any*>(src + e) : u32x4{0, 0, 0, 0};
-            }
+        for (int i = 0; i < Chunk::U; ++i) {
+            u32x4 o;
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int e = (i * GT + (int)threadIdx.x) * 8;
-                u32x4 o;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[j] = pack_bf16x2(bf16_lo(v[i][j]) * coef, bf16_hi(v[i][j]) * coef);
-                if (e + 8 <= n) *reinterpret_cast<u32x4_any*>(dst + e) = o;
-            }
-            const int e = (n & ~7) + (int)threadIdx.x;
-            if (e < n) dst[e] = (uint16_t)f32_to_bf16_rne(bf16_lo(src[e]) * coef);
-        } else {
-            const float* src = static_cast<const float*>(t.src[k]) + e0;
-            float* dst = static_cast<float*>(t.dst[k]) + e0;
-            constexpr int U = kGradChunk / (4 * GT);
-            u32x4 v[U];
-#pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int e = (i * GT + (int)threadIdx.x) * 4;
-                v[i] = e + 4 <= n ? *reinterpret_cast<const u32x4_any*>(src + e) : u32x4{0, 0, 0, 0};
-            }
-#pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int e = (i * GT + (int)threadIdx.x) * 4;
-                u32x4 o;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[j] = __float_as_uint(__uint_as_float(v[i][j]) * coef);
-                if (e + 4 <= n) *reinterpret_cast<u32x4_any*>(dst + e) = o;
-            }
-            const int e = (n & ~3) + (int)threadIdx.x;
-            if (e < n) dst[e] = src[e] * coef;
+            for (int j = 0; j < 4; ++j)
+                o[j] = now.bf16 ? pack_bf16x2(bf16_lo(now.v[i][j]) * coef, bf16_hi(now.v[i][j]) * coef)
+                                : __float_as_uint(__uint_as_float(now.v[i][j]) * coef);
+            if (now.at(i) + 16 <= now.n) *reinterpret_cast<u32x4_any*>(now.dst + now.at(i)) = o;
+        }
+        if (now.has_left) {
+            if (now.bf16) *reinterpret_cast<uint16_t*>(now.dst + now.left_at()) = (uint16_t)f32_to_bf16_rne(bf16_lo(now.left) * coef);
+            else *reinterpret_cast<float*>(now.dst + now.left_at()) = __uint_as_float(now.left) * coef;
         }
     }
 }
 
 }  // namespace
 
-hipError_t launch_grad_norm(const GradTable& t, int kind, int grid, double* partial, hipStream_t s)
+hipError_t launch_grad_norm(const GradTable& t, int kind, int grid, double* partial, GradEntry* table, hipStream_t s)
 {
-    if (kind == CBW_GRAD_NORM_2) grad_norm_kernel<SumSquares><<<grid, GT, 0, s>>>(t, partial);
-    else grad_norm_kernel<MaxAbs><<<grid, GT, 0, s>>>(t, partial);
+    if (kind == CBW_GRAD_NORM_2) grad_norm_kernel<SumSquares><<<grid, GT, 0, s>>>(t, partial, table);
+    else grad_norm_kernel<MaxAbs><<<grid, GT, 0, s>>>(t, partial, table);
     return hipGetLastError();
 }
 
@@ -228,13 +239,13 @@ hipError_t launch_grad_finish(int kind, const double* partial, int npartial, flo
     return hipGetLastError();
 }
 
-hipError_t launch_grad_scale(const GradTable& t, int kind, int grid, const double* partial, int npartial, float max_norm,
-                             float* norm, hipStream_t s)
+hipError_t launch_grad_scale(const GradEntry* table, int n, int chunks, int kind, int grid, const double* partial,
+                             int npartial, float max_norm, float* norm, hipStream_t s)
 {
     if (kind == CBW_GRAD_NORM_2)
-        grad_scale_kernel<SumSquares><<<grid, GT, 0, s>>>(t, partial, npartial, max_norm, norm);
+        grad_scale_kernel<SumSquares><<<grid, GT, 0, s>>>(table, n, chunks, partial, npartial, max_norm, norm);
     else
-        grad_scale_kernel<MaxAbs><<<grid, GT, 0, s>>>(t, partial, npartial, max_norm, norm);
+        grad_scale_kernel<MaxAbs><<<grid, GT, 0, s>>>(table, n, chunks, partial, npartial, max_norm, norm);
     return hipGetLastError();
 }
 
