@@ -288,6 +288,11 @@ def _whole(t, numel, dtype):
 def _stream(stream):
     if stream is None:
         import torch
+        # the current stream's handle, without a Stream object around it
+        # (2.5 us a call less) where this torch hands it out
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return ctypes.c_void_p(raw(torch.cuda.current_device()))
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 

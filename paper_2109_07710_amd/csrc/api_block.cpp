@@ -103,11 +103,10 @@ int64_t grad_chunks(const cbw_grad& g) { return (grad_bytes(g) + kGradChunk - 1)
 // What a call has to do: tensors with elements, and their chunks.
 struct GradWork {
     int64_t tensors, chunks;
-    // the workspace: partial sums, one more for each launch after the first
-    // (rounding), then the table of all tensors
+    // the workspace: partial sums, then the table of all tensors
     size_t partial_bytes() const
     {
-        return ((size_t)(kGradMaxWgs + (tensors + kGradTable - 1) / kGradTable) * sizeof(double) + 255) & ~(size_t)255;
+        return ((size_t)(kGradMaxWgs + (tensors + kGradTable - 1) / kGradTable * kGradMinWgs) * sizeof(double) + 255) & ~(size_t)255;
     }
     size_t ws_bytes() const { return partial_bytes() + (((size_t)tensors * sizeof(GradEntry) + 255) & ~(size_t)255); }
 };
@@ -146,10 +145,10 @@ bool next_table(const cbw_grad* grads, int32_t n, int32_t& i, GradTable& t)
     return t.n > 0;
 }
 
-// Workgroups of a launch: its share of kGradMaxWgs by chunks, at least one.
+// Workgroups of a launch: its share of kGradMaxWgs by chunks.
 int grad_grid(int64_t chunks, int64_t all)
 {
-    return (int)std::min(chunks, std::max<int64_t>(1, kGradMaxWgs * chunks / std::max<int64_t>(all, kGradMaxWgs)));
+    return (int)std::min(chunks, std::max<int64_t>(kGradMinWgs, kGradMaxWgs * chunks / std::max<int64_t>(all, 1)));
 }
 
 // Partials of all tensors into the workspace, with `table` the tensors as well; the number of partials.

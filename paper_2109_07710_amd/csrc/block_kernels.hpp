@@ -117,7 +117,8 @@ hipError_t launch_expert_bwd_weight(int dtype, const ExpertArgs& a, hipStream_t 
 
 constexpr int kGradTable = 120;       // tensors per launch: the table travels in the kernel's arguments
 constexpr int kGradChunk = 16384;     // bytes a workgroup takes at a time
-constexpr int kGradMaxWgs = 1024;     // workgroups of all launches of a pass together, one more each for rounding
+constexpr int kGradMaxWgs = 1024;     // workgroups of a pass, shared out over its launches,
+constexpr int kGradMinWgs = 256;      // of which each has this many if it has the chunks
 
 struct GradEntry {
     const void* src;

@@ -652,7 +652,7 @@ hipError_t launch_rows(const ExpertArgs& a, hipStream_t s)
     } else {
         if (mean > 16 && likely_tiles(a, 64, P, 64) >= 400) return launch_tiles<T, KIND, 64, 64, 2, 2>(a, s);
     }
-    if (mean > 64) return launch_stream<T, KIND, 64, 4, 4, 2>(a, s);
+    if (BF16 && mean > 64) return launch_stream<T, KIND, 64, 4, 4, 2>(a, s);   // (float32: the matrix unit would be the bound)
     if (likely_tiles(a, 16, P, 64) >= 192) return launch_stream<T, KIND, 64, 1, 4, 2>(a, s);
     return launch_stream<T, KIND, 32, 1, 8, 3>(a, s);
 }

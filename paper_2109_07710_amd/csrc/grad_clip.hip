@@ -106,28 +106,33 @@ __device__ __forceinline__ ChunkRange my_chunks(int chunks)
 template <typename R>
 __global__ __launch_bounds__(GT) void grad_norm_kernel(GradTable t, double* partial, GradEntry* table)
 {
+    // Kernel arguments lie far away (every first touch of a line takes a
+    // microsecond or two): the table comes to the LDS at once, not entry by
+    // entry.
+    __shared__ GradEntry e_s[kGradTable];
     const int lane = threadIdx.x & 63;
     const ChunkRange range = my_chunks(t.chunks);
+    static_assert(2 * kGradTable <= GT && sizeof(GradEntry) == 32, "a 16-byte half entry a thread");
+    if ((int)threadIdx.x < 2 * kGradTable)
+        reinterpret_cast<u32x4*>(e_s)[threadIdx.x] = reinterpret_cast<const u32x4*>(t.e)[threadIdx.x];
+    __syncthreads();
     // the tensor of the first chunk: the last one that starts at or before it
-    // (one look at all starts: a search would wait for the arguments, which
-    // lie far away, at every step)
-    const int f0 = lane < t.n ? t.e[lane].first : INT32_MAX;
-    const int f1 = lane + 64 < t.n ? t.e[lane + 64].first : INT32_MAX;
+    const int f0 = lane < t.n ? e_s[lane].first : INT32_MAX;
+    const int f1 = lane + 64 < t.n ? e_s[lane + 64 < kGradTable ? lane + 64 : 0].first : INT32_MAX;
     int k = __popcll(__ballot(f0 <= range.begin)) + __popcll(__ballot(f1 <= range.begin)) - 1;
-    static_assert(kGradTable <= 128, "two lookups a lane");
     if (table && blockIdx.x == 0 && (int)threadIdx.x < t.n) {
-        GradEntry e = t.e[threadIdx.x];
+        GradEntry e = e_s[threadIdx.x];
         e.first += t.chunk0;
         table[t.entry0 + threadIdx.x] = e;
     }
     R r;
     Chunk next;
-    next.load(t.e[k], range.begin);
+    next.load(e_s[k], range.begin);
     for (int c = range.begin; c < range.end; ++c) {
         const Chunk now = next;
         if (c + 1 < range.end) {
-            if (k + 1 < t.n && t.e[k + 1].first <= c + 1) ++k;
-            next.load(t.e[k], c + 1);
+            if (k + 1 < t.n && e_s[k + 1].first <= c + 1) ++k;
+            next.load(e_s[k], c + 1);
         }
         if (now.bf16) {
 #pragma unroll
