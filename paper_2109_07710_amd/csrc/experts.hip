@@ -21,6 +21,7 @@
 // grid covers the most tiles any lengths can give; surplus workgroups leave.
 #include "common.hpp"
 #include "block_kernels.hpp"
+#include "tiles.hpp"
 
 #include <algorithm>
 #include <type_traits>
@@ -198,8 +199,21 @@ struct Operand {
 
 // Output of the forward product and the data gradient: rows of P features,
 // `stride` elements apart, a tile's first row at offset 0.
-template <typename T, int KIND>
+//
+// A wave has 16 rows by 16 I features at a time, a lane four features of each
+// block of 16: stored so, an instruction would write 32 bytes to each of 16
+// rows (bf16).  They pass through the wave's own piece of LDS instead, and a
+// lane takes a vector of consecutive features of one row, with the footprint's
+// bits for them next to each other: an instruction writes whole lines
+// (16384 rows, 2048 -> 8192: 120 us less of 550 spent on stores).
+template <typename T, int KIND, int I>
 struct Output {
+    static constexpr int E = 16 / (int)sizeof(T);              // features of a vector
+    static constexpr int ROW = I * 16 * (int)sizeof(T);        // bytes of a row in LDS
+    static constexpr int CHUNKS = ROW / 16, VECS = I * (int)sizeof(T) / 4;
+    static constexpr int BYTES = 16 * ROW;                     // LDS per wave
+    static_assert(CHUNKS >= 4 && (CHUNKS & (CHUNKS - 1)) == 0 && 64 % CHUNKS == 0, "whole rows to an instruction");
+
     const ExpertArgs& a;
     __amdgpu_buffer_rsrc_t r;
     int64_t row0, stride;
@@ -211,39 +225,80 @@ struct Output {
         r = make_rsrc(static_cast<T*>(a.out) + row0 * stride, (uint32_t)(((rows - 1) * stride + P) * (int64_t)sizeof(T)));
     }
 
-    // Four features from p on of the tile's row q; the bits of those above
-    // zero as they are stored (the forward's footprint).
-    __device__ __forceinline__ uint32_t put(int q, int p, floatx4 v) const
+    // the row and the feature of the lane's t-th vector, from the block's first
+    static __device__ __forceinline__ int row_of(int lane, int t) { return t * (64 / CHUNKS) + lane / CHUNKS; }
+    static __device__ __forceinline__ int feature_of(int lane) { return (lane % CHUNKS) * E; }
+    // the lane's number, which the compiler takes for a new one each time: it
+    // would keep all that follows from it in registers during the products
+    static __device__ __forceinline__ int my_lane()
     {
-        const bool ok = q < rows && p < P;
-        if (KIND == FWD && a.relu)
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));
+        return lane;
+    }
+    __device__ __forceinline__ int64_t bit_of(int q, int p) const { return (row0 + q) * (int64_t)P + p; }
+
+    // The footprint's bits of the lane's vectors of rows q0 .. q0 + 15,
+    // features p0 on (data gradient).
+    struct Live {
+        uint32_t bits[VECS];
+    };
+    __device__ __forceinline__ void load_live(Live& l, int q0, int p0) const
+    {
+        const int lane = my_lane();
 #pragma unroll
-            for (int c = 0; c < 4; ++c) v[c] = v[c] > 0.f ? v[c] : 0.f;
-        if (KIND == DATA && a.mask && ok) {
-            const int64_t bit = (row0 + q) * (int64_t)P + p;
-            const uint32_t m = reinterpret_cast<const uint8_t*>(a.mask)[bit >> 3] >> (bit & 7);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) v[c] = (m >> c) & 1u ? v[c] : 0.f;
+        for (int t = 0; t < VECS; ++t) {
+            const int q = q0 + row_of(lane, t), p = p0 + feature_of(lane);
+            l.bits[t] = ~0u;
+            if (KIND == DATA && a.mask && q < rows && p < P)
+                l.bits[t] = reinterpret_cast<const uint8_t*>(a.mask)[bit_of(q, p) >> 3] >> (bit_of(q, p) & 7);
         }
-        const uint32_t off = ok ? (uint32_t)(q * stride + p) * (uint32_t)sizeof(T) : kOOB;
-        if (sizeof(T) == 4) {
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, off, 0, 0);
-            return KIND == FWD ? (v[0] > 0.f) | (v[1] > 0.f) << 1 | (v[2] > 0.f) << 2 | (v[3] > 0.f) << 3 : 0;
-        }
-        const u32x2 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-        __builtin_amdgcn_raw_buffer_store_b64(w, r, off, 0, 0);
-        // (after ReLU a stored value is positive unless its bits are zero)
-        return KIND == FWD ? ((w.x & 0xffffu) != 0) | ((w.x >> 16) != 0) << 1 | ((w.y & 0xffffu) != 0) << 2 | ((w.y >> 16) != 0) << 3 : 0;
     }
 
-    // Footprint word of the 32 features from p on of row q, from the lanes'
-    // four bits of its two blocks of 16 features.
-    __device__ __forceinline__ void put_bits(int q, int p, uint32_t lo, uint32_t hi) const
+    // v[i]: the lane's four features of block i of rows q0 .. q0 + 15.
+    template <typename V>
+    __device__ __forceinline__ void put(char* lds, int q0, int p0, const V& v, const Live& live) const
     {
-        uint32_t w = (lo | hi << 16) << (4 * ((threadIdx.x & 63) >> 4));
-        w |= __shfl_xor(w, 16);
-        w |= __shfl_xor(w, 32);
-        if ((threadIdx.x & 63) < 16 && q < rows && p < P) a.out_mask[((row0 + q) * (int64_t)P + p) >> 5] = w;
+        const int lane = my_lane(), row = lane & 15;
+        // (a row's chunks are moved by its number: the 16 rows' do not share banks)
+        auto at = [&](int rr, int chunk) { return lds + rr * ROW + ((chunk ^ (rr & (CHUNKS - 1))) << 4); };
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            floatx4 x = v(i);
+            if (KIND == FWD && a.relu)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) x[c] = x[c] > 0.f ? x[c] : 0.f;
+            if (sizeof(T) == 2)
+                *reinterpret_cast<u32x2*>(at(row, i * 2 + (lane >> 5)) + (lane >> 4 & 1) * 8) =
+                    u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+            else
+                *reinterpret_cast<u32x4*>(at(row, i * 4 + (lane >> 4))) = __builtin_bit_cast(u32x4, x);
+        }
+#pragma unroll
+        for (int t = 0; t < VECS; ++t) {
+            const int rr = row_of(lane, t), q = q0 + rr, p = p0 + feature_of(lane);
+            const bool ok = q < rows && p < P;
+            u32x4 w = *reinterpret_cast<const u32x4*>(at(rr, lane % CHUNKS));
+            if (KIND == DATA) {
+                const uint32_t b = live.bits[t];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    w[k] &= sizeof(T) == 2 ? ((b >> 2 * k) & 1u ? 0xffffu : 0u) | ((b >> (2 * k + 1)) & 1u ? 0xffff0000u : 0u)
+                                           : ((b >> k) & 1u ? ~0u : 0u);
+            }
+            __builtin_amdgcn_raw_buffer_store_b128(w, r, ok ? (uint32_t)(q * stride + p) * (uint32_t)sizeof(T) : kOOB, 0, 0);
+            if (KIND == FWD && a.out_mask) {
+                // (after ReLU a stored value is positive unless its bits are zero)
+                uint32_t b = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    b |= sizeof(T) == 2 ? (uint32_t)((w[k] & 0xffffu) != 0) << 2 * k | (uint32_t)((w[k] >> 16) != 0) << (2 * k + 1)
+                                        : (uint32_t)(w[k] != 0) << k;
+                if (sizeof(T) == 4) b |= __shfl_xor(b, 1) << 4;   // (the even lane's four features are the lower half)
+                if (ok && (sizeof(T) == 2 || (lane & 1) == 0))
+                    reinterpret_cast<uint8_t*>(a.out_mask)[bit_of(q, p) >> 3] = (uint8_t)b;
+            }
+        }
     }
 };
 
@@ -258,101 +313,118 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
     constexpr int KB = OP::KB, COPIES = OP::COPIES + OQ::COPIES;
     __shared__ __align__(1024) char lds_p[2][OP::BYTES];
     __shared__ __align__(1024) char lds_q[2][OQ::BYTES];
+    using Out = Output<T, KIND, FM>;
+    __shared__ __align__(1024) char lds_out[KIND == WEIGHT ? 1 : NW][KIND == WEIGHT ? 16 : Out::BYTES];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wp = wave / NWQ, wq = wave % NWQ;
 
-    // the workgroup's tile
+    // A tile's place: its expert, the first of its rows (weight: of the part's)
+    // and how many, its first columns, its reduction indices.
+    struct Tile {
+        int e, within, p0, q0;
+        int64_t row0, len;
+        int qrows;
+    };
     const int P = KIND == FWD ? a.K : a.C;                     // features of the output
     const int ptiles = (P + TP - 1) / TP, qtiles = KIND == WEIGHT ? (a.K + TQ - 1) / TQ : 1;
-    int unit, pt, qt = 0, within, e;
-    if (KIND == WEIGHT) {
-        // Units are experts, or parts of one, of very different lengths: every
-        // XCD takes an equal share of the tiles of each (contiguous, so that
-        // they share operands), the shares turning from unit to unit.
-        const int per = ptiles * qtiles, share = (per + 7) >> 3;
-        const int j = blockIdx.x >> 3;
-        unit = j / share;
-        const int t = (((int)blockIdx.x + unit) & 7) * share + j - unit * share;
-        if (t >= per) return;
-        pt = t / qtiles;
-        qt = t - pt * qtiles;
-        auto parts = [&](const Group& g) { return (int)max((g.count + a.split_rows - 1) / a.split_rows, (int64_t)1); };
-        e = number_units(a, parts).find(unit, within);
-    } else {
-        auto units = [&](const Group& g) { return (int)((g.count + TQ - 1) / TQ); };
-        auto all = number_units(a, units);
-        const int nunits = all.total, total = nunits * ptiles;
-        if ((int)blockIdx.x >= total) return;
-        const int b = xcd_remap(blockIdx.x, total);
-        // blocks of eight row tiles by all feature tiles, so that the tiles
+    // units of work: row tiles, or (weight) experts and parts of one
+    auto all = number_units(a, [&](const Group& g) {
+        return KIND == WEIGHT ? (int)max((g.count + a.split_rows - 1) / a.split_rows, (int64_t)1) : (int)((g.count + TQ - 1) / TQ);
+    });
+    const int total = all.total * ptiles;                      // (row tiles)
+    auto place = [&](int unit, int pt, int qt) {
+        Tile t;
+        int within;
+        t.e = __builtin_amdgcn_readfirstlane(all.find(unit, within));
+        t.within = __builtin_amdgcn_readfirstlane(within);
+        if (t.e < 0) return t;
+        const Group g = group_of(a, t.e);
+        t.p0 = pt * TP;
+        t.q0 = qt * TQ;
+        t.row0 = g.first + (int64_t)t.within * (KIND == WEIGHT ? a.split_rows : TQ);
+        const int64_t left = g.first + g.count - t.row0;
+        t.qrows = KIND == WEIGHT ? 0 : (int)min((int64_t)TQ, left);
+        t.len = KIND == WEIGHT ? min((int64_t)a.split_rows, left) : KIND == FWD ? a.C : a.K;
+        return t;
+    };
+    // The workgroup's `turn`-th tile; e < 0: there is none.
+    auto tile_of = [&](int turn) {
+        Tile none;
+        none.e = -1;
+        if (KIND == WEIGHT) {
+            // Units of very different lengths: every XCD takes an equal share
+            // of the tiles of each (contiguous, so that they share operands),
+            // the shares turning from unit to unit.
+            const int per = ptiles * qtiles, share = (per + 7) >> 3;
+            const int j = blockIdx.x >> 3, unit = j / share;
+            const int t = (((int)blockIdx.x + unit) & 7) * share + j - unit * share;
+            if (turn > 0 || t >= per) return none;
+            return place(unit, t / qtiles, t % qtiles);
+        }
+        // Blocks of eight row tiles by all feature tiles, so that the tiles
         // that run at one time share both operands in the cache (four: 2 to
-        // 10% slower at 16384 rows, 2048 -> 8192 features, 8 experts)
+        // 10% slower at 16384 rows, 2048 -> 8192 features, 8 experts); a turn
+        // is a contiguous range, and an XCD's part of it is one as well.
         constexpr int GR = 8;
+        const int first = turn * (int)gridDim.x, n = min((int)gridDim.x, total - first);
+        if ((int)blockIdx.x >= n) return none;
+        const int b = first + xcd_remap(blockIdx.x, n);
         const int blk = b / (GR * ptiles), in_blk = b - blk * GR * ptiles;
-        const int h = min(GR, nunits - blk * GR);
-        pt = in_blk / h;
-        unit = blk * GR + in_blk - pt * h;
-        e = all.find(unit, within);
-    }
-    e = __builtin_amdgcn_readfirstlane(e);
-    if (e < 0) return;
-    const Group g = group_of(a, e);
-    within = __builtin_amdgcn_readfirstlane(within);
-    const int p0 = pt * TP, q0 = qt * TQ;
+        const int h = min(GR, all.total - blk * GR);
+        const int pt = in_blk / h;
+        return place(blk * GR + in_blk - pt * h, pt, 0);
+    };
+
+    Tile t = tile_of(0);
+    if (t.e < 0) return;
 
     OP op;
     OQ oq;
-    int64_t row0 = 0;       // first row of the tile (weight: of the part)
-    int64_t len;            // reduction indices
-    int64_t qrows = 0;
     const char *base_p, *base_q;
-    if (KIND == WEIGHT) {
-        row0 = g.first + (int64_t)within * a.split_rows;
-        len = min((int64_t)a.split_rows, g.first + g.count - row0);
-        base_p = reinterpret_cast<const char*>(static_cast<const T*>(a.p) + row0 * a.x_stride + p0);
-        base_q = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + row0 * a.y_stride + q0);
-        op.init(wave, a.C - p0, a.x_stride);
-        oq.init(wave, a.K - q0, a.y_stride);
-    } else {
-        const int64_t qstride = KIND == FWD ? a.x_stride : a.y_stride;
-        const T* w = static_cast<const T*>(a.p) + (int64_t)e * a.K * a.C;
-        row0 = g.first + (int64_t)within * TQ;
-        qrows = min((int64_t)TQ, g.first + g.count - row0);
-        len = KIND == FWD ? a.C : a.K;
-        base_p = reinterpret_cast<const char*>(w + (KIND == FWD ? (int64_t)p0 * a.C : (int64_t)p0));
-        base_q = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + row0 * qstride);
-        op.init(wave, KIND == FWD ? 0 : a.C - p0, a.C);
-        oq.init(wave, 0, qstride);
-    }
-
-    auto copy = [&](int64_t k, int buf) {
-        const int64_t left = min(len - k, (int64_t)KB);
+    auto aim = [&](const Tile& t) {
+        if (KIND == WEIGHT) {
+            base_p = reinterpret_cast<const char*>(static_cast<const T*>(a.p) + t.row0 * a.x_stride + t.p0);
+            base_q = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + t.row0 * a.y_stride + t.q0);
+            op.init(wave, a.C - t.p0, a.x_stride);
+            oq.init(wave, a.K - t.q0, a.y_stride);
+        } else {
+            const int64_t qstride = KIND == FWD ? a.x_stride : a.y_stride;
+            const T* w = static_cast<const T*>(a.p) + (int64_t)t.e * a.K * a.C;
+            base_p = reinterpret_cast<const char*>(w + (KIND == FWD ? (int64_t)t.p0 * a.C : (int64_t)t.p0));
+            base_q = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + t.row0 * qstride);
+            op.init(wave, KIND == FWD ? 0 : a.C - t.p0, a.C);
+            oq.init(wave, 0, qstride);
+        }
+    };
+    auto copy = [&](const Tile& t, int64_t k, int buf) {
+        const int64_t left = min(t.len - k, (int64_t)KB);
         // (an operand that goes across: the step's rows, the last of which ends with its own columns)
         if (KIND == FWD) {
-            const uint32_t n = (uint32_t)min(TP, a.K - p0) * (uint32_t)a.C * sizeof(T);
-            op.copy(wave, make_rsrc_words(base_p, n), (int)k, (int)len, lds_p[buf]);
+            const uint32_t n = (uint32_t)min(TP, a.K - t.p0) * (uint32_t)a.C * sizeof(T);
+            op.copy(wave, make_rsrc_words(base_p, n), (int)k, (int)t.len, lds_p[buf]);
         } else {
             const int64_t stride = KIND == WEIGHT ? a.x_stride : (int64_t)a.C;
-            const uint32_t n = (uint32_t)(((left - 1) * stride + a.C - p0) * (int64_t)sizeof(T));
+            const uint32_t n = (uint32_t)(((left - 1) * stride + a.C - t.p0) * (int64_t)sizeof(T));
             op.copy(wave, make_rsrc_words(base_p + k * stride * (int64_t)sizeof(T), n), 0, 0, lds_p[buf]);
         }
         if (KIND == WEIGHT) {
-            const uint32_t n = (uint32_t)(((left - 1) * a.y_stride + a.K - q0) * (int64_t)sizeof(T));
+            const uint32_t n = (uint32_t)(((left - 1) * a.y_stride + a.K - t.q0) * (int64_t)sizeof(T));
             oq.copy(wave, make_rsrc_words(base_q + k * a.y_stride * (int64_t)sizeof(T), n), 0, 0, lds_q[buf]);
         } else {
             const int64_t stride = KIND == FWD ? a.x_stride : a.y_stride;
-            const uint32_t n = (uint32_t)(((qrows - 1) * stride + len) * (int64_t)sizeof(T));
-            oq.copy(wave, make_rsrc_words(base_q, n), (int)k, (int)len, lds_q[buf]);
+            const uint32_t n = (uint32_t)(((t.qrows - 1) * stride + t.len) * (int64_t)sizeof(T));
+            oq.copy(wave, make_rsrc_words(base_q, n), (int)k, (int)t.len, lds_q[buf]);
         }
+    };
+    // the first two steps' copies of a tile
+    auto start = [&](const Tile& t) {
+        aim(t);
+        if (t.len > 0) copy(t, 0, 0);
+        if (t.len > KB) copy(t, KB, 1);
     };
 
     floatx4 acc[FM][FN];
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-
     // Fragments of a step's two halves in turn: while the matrix instructions of
     // one run, the reads of the next are under way, so that the LDS latency is
     // under them and not behind the barrier.  The barrier stands between the
@@ -384,54 +456,58 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
             __builtin_amdgcn_sched_group_barrier(0x008, MUL / READS, 0);          // matrix instructions
         }
     };
-    const int steps = (int)((len + KB - 1) / KB);
     Fragments fa, fb;
-    if (steps > 0) {
-        copy(0, 0);
-        if (steps > 1) {
-            copy(KB, 1);
-            wait_copies<COPIES>();
-        } else {
-            wait_copies<0>();
-        }
+    auto product = [&](const Tile& t) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+        const int steps = (int)((t.len + KB - 1) / KB);
+        if (steps == 0) return;
+        if (steps > 1) wait_copies<COPIES>();
+        else wait_copies<0>();
         barrier();
         read(fa, 0, 0);
-    }
-    for (int s = 0; s < steps; ++s) {
-        const int buf = s & 1;
-        read(fb, buf, 1);
-        multiply(fa);
-        interleave();
-        wait_copies<0>();
-        wait_reads();
-        barrier();
-        if (s + 2 < steps) copy((int64_t)(s + 2) * KB, buf);
-        read(fa, buf ^ 1, 0);   // (after the last step: what was there, unused)
-        multiply(fb);
-        interleave();
-    }
+        for (int s = 0; s < steps; ++s) {
+            const int buf = s & 1;
+            read(fb, buf, 1);
+            multiply(fa);
+            interleave();
+            wait_copies<0>();
+            wait_reads();
+            barrier();
+            if (s + 2 < steps) copy(t, (int64_t)(s + 2) * KB, buf);
+            read(fa, buf ^ 1, 0);   // (after the last step: what was there, unused)
+            multiply(fb);
+            interleave();
+        }
+    };
 
-    const int pl = p0 + wp * (TP / NWP) + 4 * (lane >> 4), ql = wq * (TQ / NWQ) + (lane & 15);
+    const int pw = wp * (TP / NWP), ql = wq * (TQ / NWQ) + (lane & 15);
     if (KIND == WEIGHT) {
+        start(t);
+        product(t);
         float* out = nullptr;
-        if (g.count > a.split_rows) {
+        const int64_t count = group_of(a, t.e).count;
+        if (count > a.split_rows) {
             // the expert's slots follow those of the split experts before it
             auto slots = [&](const Group& gg) {
                 return gg.count > a.split_rows ? (int)((gg.count + a.split_rows - 1) / a.split_rows) : 0;
             };
             int before = 0;
-            for (int e0 = 0; e0 < e; e0 += 64) {
+            for (int e0 = 0; e0 < t.e; e0 += 64) {
                 const int x = e0 + lane;
-                before += __builtin_amdgcn_readlane(wave_inclusive_sum(x < e ? slots(group_of(a, x)) : 0), 63);
+                before += __builtin_amdgcn_readlane(wave_inclusive_sum(x < t.e ? slots(group_of(a, x)) : 0), 63);
             }
-            if (before + within < a.slots) out = a.partial + (int64_t)(before + within) * a.K * a.C;   // (offsets that decrease)
+            if (before + t.within < a.slots) out = a.partial + (int64_t)(before + t.within) * a.K * a.C;   // (offsets that decrease)
         } else {
-            out = static_cast<float*>(a.out) + (int64_t)e * a.K * a.C;
+            out = static_cast<float*>(a.out) + (int64_t)t.e * a.K * a.C;
         }
         const __amdgpu_buffer_rsrc_t r = make_rsrc(out, out ? (uint32_t)a.K * (uint32_t)a.C * 4u : 0u);
+        const int pl = t.p0 + pw + 4 * (lane >> 4);
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const int k = q0 + ql + j * 16;
+            const int k = t.q0 + ql + j * 16;
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
                 // non-temporal: the gradients are not read again here, and as
@@ -443,16 +519,29 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
         }
         return;
     }
-    const Output<T, KIND> out(a, row0, (int)qrows);
-    const bool bits = KIND == FWD && a.out_mask;
+    // A workgroup stays for all its tiles: the next one's first copies are
+    // under way while a finished one is stored.  (One tile to a workgroup: 14
+    // us from a tile's last product to the next one's first, of 61 us a tile at
+    // 2048 reduction indices.)
+    start(t);
+    for (int turn = 1;; ++turn) {
+        const Tile next = tile_of(turn);
+        product(t);
+        const Out out(a, t.row0, t.qrows);
+        typename Out::Live live[FN];
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int i = 0; i < FM; i += 2) {
-            const uint32_t lo = out.put(ql + j * 16, pl + i * 16, acc[i][j]);
-            const uint32_t hi = out.put(ql + j * 16, pl + i * 16 + 16, acc[i + 1][j]);
-            if (bits) out.put_bits(ql + j * 16, p0 + wp * (TP / NWP) + i * 16, lo, hi);
+        for (int j = 0; j < FN; ++j) out.load_live(live[j], wq * (TQ / NWQ) + j * 16, t.p0 + pw);
+        if (next.e >= 0) {
+            wait_reads();
+            barrier();   // every wave is done with both buffers
+            start(next);
         }
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            out.put(lds_out[wave], wq * (TQ / NWQ) + j * 16, t.p0 + pw, [&](int i) { return acc[i][j]; }, live[j]);
+        if (next.e < 0) return;
+        t = next;
+    }
 }
 
 // Few rows to an expert (serving, or many experts): bound by reading the
@@ -467,8 +556,8 @@ __global__ __launch_bounds__(NW * 64) void expert_stream_kernel(ExpertArgs a)
     using OP = Operand<T, TP, KIND != FWD, 1>;
     using OQ = Operand<T, TQ, false, 1>;
     constexpr int KB = OP::KB, COPIES = OP::COPIES + OQ::COPIES, STAGE = OP::BYTES + OQ::BYTES;
-    constexpr int SUMS = NW * FM * FN * 1024;
-    __shared__ __align__(1024) char lds[NW * RING * STAGE > SUMS ? NW * RING * STAGE : SUMS];
+    constexpr int SUMS = NW * FM * FN * 1024, OUT = 16 * TP * (int)sizeof(T);
+    __shared__ __align__(1024) char lds[NW * RING * STAGE > SUMS + FN * OUT ? NW * RING * STAGE : SUMS + FN * OUT];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int P = KIND == FWD ? a.K : a.C, ptiles = (P + TP - 1) / TP;
@@ -556,17 +645,19 @@ __global__ __launch_bounds__(NW * 64) void expert_stream_kernel(ExpertArgs a)
 #pragma unroll
         for (int j = 0; j < FN; ++j) sums[(wave * FM * FN + i * FN + j) * 64 + lane] = acc[i][j];
     __syncthreads();
-    const Output<T, KIND> out(a, row0, qrows);
-    for (int u = wave; u < FM / 2 * FN; u += NW) {
-        const int i = u / FN * 2, j = u % FN;
-        floatx4 v[2] = {};
+    // a wave adds up 16 rows of all features at a time and stores them
+    using Out = Output<T, KIND, FM>;
+    const Out out(a, row0, qrows);
+    static_assert(Out::BYTES <= OUT, "room for a wave's rows");
+    for (int j = wave; j < FN; j += NW) {
+        floatx4 v[FM] = {};
 #pragma unroll
         for (int z = 0; z < NW; ++z)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) v[k] += sums[(z * FM * FN + (i + k) * FN + j) * 64 + lane];
-        const int q = j * 16 + (lane & 15), p = p0 + i * 16 + 4 * (lane >> 4);
-        const uint32_t lo = out.put(q, p, v[0]), hi = out.put(q, p + 16, v[1]);
-        if (KIND == FWD && a.out_mask) out.put_bits(q, p0 + i * 16, lo, hi);
+            for (int i = 0; i < FM; ++i) v[i] += sums[(z * FM * FN + i * FN + j) * 64 + lane];
+        typename Out::Live live;
+        out.load_live(live, j * 16, p0);
+        out.put(lds + SUMS + j * OUT, j * 16, p0, [&](int i) { return v[i]; }, live);
     }
 }
 
@@ -607,7 +698,9 @@ hipError_t launch_tiles(const ExpertArgs& a, hipStream_t s)
     const int64_t grid = KIND == WEIGHT ? (a.rows / a.split_rows + a.E) * ((per + 7) / 8 * 8) : most_units(a.rows, a.E, TQ) * per;
     if (grid == 0) return hipSuccess;
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
-    expert_kernel<T, KIND, TP, TQ, NWP, NWQ><<<(int)grid, NWP * NWQ * 64, 0, s>>>(a);
+    // as many workgroups as are resident (by their LDS), where they stay for several tiles
+    const int64_t resident = (int64_t)CBW_NUM_CUS * (163840 / ((TP + TQ) * 256 + TP * TQ / (TQ / NWQ / 16) * (int)sizeof(T)));
+    expert_kernel<T, KIND, TP, TQ, NWP, NWQ><<<(int)(KIND == WEIGHT ? grid : std::min(grid, resident)), NWP * NWQ * 64, 0, s>>>(a);
     return hipGetLastError();
 }
 
