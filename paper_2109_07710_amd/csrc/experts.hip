@@ -146,54 +146,83 @@ struct Operand {
         return 2 * ((line >> 3) & 1);
     }
 
-    uint32_t off[COPIES];   // byte offset of the lane's 16 bytes at step 0, kOOB: never valid
-    int k0[2];              // along: the lane's first reduction index at step 0, in even and odd copies
+    // Copies DIST apart lie a multiple of 16 LDS rows apart, which the swizzle
+    // does not see: the same lane has the same chunk, so its byte offset grows
+    // by a uniform amount.
+    static constexpr int LINES_PER_COPY = NW * 64 / CHUNKS;
+    static constexpr int DIST = LINES_PER_COPY % 16 == 0 ? 1 : 16 / LINES_PER_COPY;
+    static_assert(COPIES < DIST || COPIES % DIST == 0, "every distinct copy as often");
+    static constexpr int OWN = COPIES < DIST ? COPIES : DIST;
+
+    uint32_t off[OWN];   // byte offset of the lane's 16 bytes at step 0, kOOB: never valid
+    uint32_t apart;      // (uniform) bytes from a copy to the one DIST further
 
     // along: rows of `stride` elements; across: `n` valid columns
-    __device__ void init(int wave, int64_t n, int64_t stride)
+    __device__ __forceinline__ void init(int wave, int64_t n, int64_t stride)
     {
         const int lane = threadIdx.x & 63;
 #pragma unroll
-        for (int j = 0; j < COPIES; ++j) {
+        for (int j = 0; j < OWN; ++j) {
             const int at = (wave + NW * j) * 64 + lane;
             const int line = at / CHUNKS, lc = (at % CHUNKS) ^ swizzle(line);
             off[j] = ACROSS && lc * E >= n ? kOOB : (uint32_t)(line * stride + lc * E) * ESZ;
-            if (j < 2) k0[j] = lc * E;   // (two copies, 16 rows or more, further it is the same)
         }
-        if (COPIES == 1) k0[1] = k0[0];
+        apart = (uint32_t)(DIST * LINES_PER_COPY * stride) * ESZ;
     }
 
     // Copy of a step's tile to LDS.  along: reduction indices from `k` on, of
     // `len`; across: the descriptor already starts at the step's first row.
     __device__ __forceinline__ void copy(int wave, const u32x4_t& rsrc, int k, int len, char* lds) const
     {
-        const uint32_t kill0 = ACROSS || k + k0[0] < len ? 0u : kOOB, kill1 = ACROSS || k + k0[1] < len ? 0u : kOOB;
+        const int lane = threadIdx.x & 63;
 #pragma unroll
-        for (int j = 0; j < COPIES; ++j)
-            buf_load16_lds(rsrc, ACROSS ? off[j] : (off[j] + (uint32_t)k * ESZ) | (j & 1 ? kill1 : kill0),
-                           lds_addr(lds + (wave + NW * j) * 1024));
+        for (int j = 0; j < COPIES; ++j) {
+            uint32_t o = off[j % OWN] + (uint32_t)(j / OWN) * apart;
+            if (!ACROSS) {
+                // (only a last, short step has indices to leave out)
+                const int lc = (lane % CHUNKS) ^ swizzle(((wave + NW * (j % OWN)) * 64 + lane) / CHUNKS);
+                o += (uint32_t)k * ESZ;
+                if (k + KB > len && k + lc * E >= len) o = kOOB;
+            }
+            buf_load16_lds(rsrc, o, lds_addr(lds + (wave + NW * j) * 1024));
+        }
     }
 
-    // The 16-wide fragment of columns cb .. cb+15 at the ks-th 64-byte part of
-    // a step (32 bf16 or 16 float32 reduction indices).
-    static __device__ __forceinline__ uint4 fragment(const char* lds, int cb, int ks)
+    // Fragments of the F blocks of 16 columns from cb on (a multiple of 16 F), at
+    // the ks-th 64-byte part of a step (32 bf16 or 16 float32 reduction
+    // indices).  Within a tile a fragment's place differs from the first one's
+    // by bits that the swizzle leaves to a plain exclusive or, so that one
+    // register serves all of them: kept apart they would fill the registers of
+    // the 256 x 256 tile.
+    static __device__ __forceinline__ int first(int cb)
     {
         const int lane = threadIdx.x & 63;
-        if (!ACROSS) {
-            const int row = cb + (lane & 15);
-            return *reinterpret_cast<const uint4*>(lds + row * 128 + (((ks * 4 + (lane >> 4)) ^ swizzle(row)) << 4));
-        }
+        if (!ACROSS) return (cb + (lane & 15)) * 128 + (((lane >> 4) ^ swizzle(lane & 15)) << 4);
         if (ESZ == 2) {
-            const int line = ks * 32 + 8 * (lane >> 4) + ((lane >> 2) & 3), col = cb + 4 * (lane & 3);
-            auto at = [&](int r) { return lds + r * (N * 2) + (((col >> 3) ^ swizzle(r)) << 4) + ((col & 7) << 1); };
-            const uint2 lo = lds_read_transposed(at(line)), hi = lds_read_transposed(at(line + 4));
-            return make_uint4(lo.x, lo.y, hi.x, hi.y);
+            const int line = 8 * (lane >> 4) + ((lane >> 2) & 3), col = cb + 4 * (lane & 3);
+            return line * (N * 2) + (((col >> 3) ^ swizzle(line)) << 4) + ((col & 7) << 1);
         }
-        const int line = ks * 16 + 4 * (lane >> 4), col = cb + (lane & 15);
-        auto at = [&](int r) {
-            return *reinterpret_cast<const uint32_t*>(lds + r * (N * 4) + (((col >> 2) ^ swizzle(r)) << 4) + ((col & 3) << 2));
-        };
-        return make_uint4(at(line), at(line + 1), at(line + 2), at(line + 3));
+        const int line = 4 * (lane >> 4), col = cb + (lane & 15);
+        return line * (N * 4) + (((col >> 2) ^ swizzle(line)) << 4) + ((col & 3) << 2);
+    }
+    template <int F>
+    static __device__ __forceinline__ void fragments(const char* lds, int at, int ks, uint4 (&f)[F])
+    {
+        static_assert((F & (F - 1)) == 0, "a power of two");
+        asm volatile("" : "+v"(at));   // (not to be worked out ahead for every block)
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            if (!ACROSS) {
+                f[i] = *reinterpret_cast<const uint4*>(lds + (at ^ (ks * 64)) + i * 2048);
+            } else if (ESZ == 2) {
+                const char* p = lds + (at ^ (i * 32)) + ks * 64 * N;
+                const uint2 lo = lds_read_transposed(p), hi = lds_read_transposed(p + 8 * N);
+                f[i] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            } else {
+                const uint32_t* p = reinterpret_cast<const uint32_t*>(lds + (at ^ (i * 64)) + ks * 64 * N);
+                f[i] = make_uint4(p[0], p[N], p[2 * N], p[3 * N]);
+            }
+        }
     }
 };
 
@@ -238,26 +267,26 @@ struct Output {
     }
     __device__ __forceinline__ int64_t bit_of(int q, int p) const { return (row0 + q) * (int64_t)P + p; }
 
-    // The footprint's bits of the lane's vectors of rows q0 .. q0 + 15,
-    // features p0 on (data gradient).
-    struct Live {
-        uint32_t bits[VECS];
-    };
-    __device__ __forceinline__ void load_live(Live& l, int q0, int p0) const
+    // The footprint of rows q0 .. q0 + 15, features p0 on (data gradient): where
+    // its rows are whole words, a word to a lane, row by row.
+    __device__ __forceinline__ bool words() const { return (P & 31) == 0; }
+    __device__ __forceinline__ uint32_t load_live(int q0, int p0) const
     {
-        const int lane = my_lane();
-#pragma unroll
-        for (int t = 0; t < VECS; ++t) {
-            const int q = q0 + row_of(lane, t), p = p0 + feature_of(lane);
-            l.bits[t] = ~0u;
-            if (KIND == DATA && a.mask && q < rows && p < P)
-                l.bits[t] = reinterpret_cast<const uint8_t*>(a.mask)[bit_of(q, p) >> 3] >> (bit_of(q, p) & 7);
-        }
+        if (KIND != DATA || !a.mask || !words()) return 0;
+        const int lane = my_lane(), q = q0 + lane / (I / 2), p = p0 + lane % (I / 2) * 32;
+        return lane < 8 * I && q < rows && p < P ? a.mask[bit_of(q, p) >> 5] : 0u;
+    }
+    // the bits of the lane's vector of row rr
+    __device__ __forceinline__ uint32_t live_bits(uint32_t word, int lane, int rr, int q, int p) const
+    {
+        if (!a.mask) return ~0u;
+        if (words()) return __shfl(word, rr * (I / 2) + feature_of(lane) / 32) >> (feature_of(lane) % 32);
+        return q < rows && p < P ? reinterpret_cast<const uint8_t*>(a.mask)[bit_of(q, p) >> 3] >> (bit_of(q, p) & 7) : 0u;
     }
 
     // v[i]: the lane's four features of block i of rows q0 .. q0 + 15.
     template <typename V>
-    __device__ __forceinline__ void put(char* lds, int q0, int p0, const V& v, const Live& live) const
+    __device__ __forceinline__ void put(char* lds, int q0, int p0, const V& v, uint32_t live) const
     {
         const int lane = my_lane(), row = lane & 15;
         // (a row's chunks are moved by its number: the 16 rows' do not share banks)
@@ -280,7 +309,7 @@ struct Output {
             const bool ok = q < rows && p < P;
             u32x4 w = *reinterpret_cast<const u32x4*>(at(rr, lane % CHUNKS));
             if (KIND == DATA) {
-                const uint32_t b = live.bits[t];
+                const uint32_t b = live_bits(live, lane, rr, q, p);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     w[k] &= sizeof(T) == 2 ? ((b >> 2 * k) & 1u ? 0xffffu : 0u) | ((b >> (2 * k + 1)) & 1u ? 0xffff0000u : 0u)
@@ -434,11 +463,10 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
     struct Fragments {
         uint4 p[FM], q[FN];
     };
+    const int frag_p = OP::first(wp * (TP / NWP)), frag_q = OQ::first(wq * (TQ / NWQ));
     auto read = [&](Fragments& f, int buf, int ks) {
-#pragma unroll
-        for (int j = 0; j < FN; ++j) f.q[j] = OQ::fragment(lds_q[buf], wq * (TQ / NWQ) + j * 16, ks);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) f.p[i] = OP::fragment(lds_p[buf], wp * (TP / NWP) + i * 16, ks);
+        OQ::fragments(lds_q[buf], frag_q, ks, f.q);
+        OP::fragments(lds_p[buf], frag_p, ks, f.p);
     };
     auto multiply = [&](const Fragments& f) {
 #pragma unroll
@@ -528,9 +556,9 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
         const Tile next = tile_of(turn);
         product(t);
         const Out out(a, t.row0, t.qrows);
-        typename Out::Live live[FN];
+        uint32_t live[FN];
 #pragma unroll
-        for (int j = 0; j < FN; ++j) out.load_live(live[j], wq * (TQ / NWQ) + j * 16, t.p0 + pw);
+        for (int j = 0; j < FN; ++j) live[j] = out.load_live(wq * (TQ / NWQ) + j * 16, t.p0 + pw);
         if (next.e >= 0) {
             wait_reads();
             barrier();   // every wave is done with both buffers
@@ -589,6 +617,7 @@ __global__ __launch_bounds__(NW * 64) void expert_stream_kernel(ExpertArgs a)
     op.init(0, KIND == FWD ? 0 : a.C - p0, a.C);
     oq.init(0, 0, qstride);
     char* ring = lds + wave * RING * STAGE;
+    const int frag_p = OP::first(0), frag_q = OQ::first(0);
 
     auto copy = [&](int step, int slot) {
         const int64_t k = (int64_t)step * KB;
@@ -622,10 +651,8 @@ __global__ __launch_bounds__(NW * 64) void expert_stream_kernel(ExpertArgs a)
         uint4 fp[2][FM], fq[2][FN];
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-#pragma unroll
-            for (int j = 0; j < FN; ++j) fq[ks][j] = OQ::fragment(lq, j * 16, ks);
-#pragma unroll
-            for (int i = 0; i < FM; ++i) fp[ks][i] = OP::fragment(lp, i * 16, ks);
+            OQ::fragments(lq, frag_q, ks, fq[ks]);
+            OP::fragments(lp, frag_p, ks, fp[ks]);
         }
         wait_reads();
         if (t + RING < steps) copy(wave + (t + RING) * NW, slot);
@@ -655,9 +682,7 @@ __global__ __launch_bounds__(NW * 64) void expert_stream_kernel(ExpertArgs a)
         for (int z = 0; z < NW; ++z)
 #pragma unroll
             for (int i = 0; i < FM; ++i) v[i] += sums[(z * FM * FN + i * FN + j) * 64 + lane];
-        typename Out::Live live;
-        out.load_live(live, j * 16, p0);
-        out.put(lds + SUMS + j * OUT, j * 16, p0, [&](int i) { return v[i]; }, live);
+        out.put(lds + SUMS + j * OUT, j * 16, p0, [&](int i) { return v[i]; }, out.load_live(j * 16, p0));
     }
 }
 
