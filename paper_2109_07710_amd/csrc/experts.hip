@@ -57,17 +57,31 @@ __device__ __forceinline__ int wave_inclusive_sum(int v)
 
 // The work of all experts, numbered through: expert e has units(e's group) of
 // it.  Up to 64 experts a lane keeps its expert's numbers; more are gone
-// through 64 at a time, again for every question.  Called by whole waves;
+// through 64 at a time, again for every question.  SORTED: up to 64 experts go
+// by their rows, most first, more stay as they are.  Called by whole waves;
 // every result is the same in all lanes.
-template <typename F>
+template <bool SORTED, typename F>
 struct Units {
     const ExpertArgs& a;
     F units;
-    int n, incl, total;   // of the lane's expert; of all
+    int e, n, incl, total;   // the lane's expert and its units; of all
 
     __device__ Units(const ExpertArgs& args, F f) : a(args), units(f)
     {
         total = 0;
+        if (SORTED && a.E <= 64) {
+            const int lane = threadIdx.x & 63;
+            const int rows = lane < a.E ? (int)group_of(a, lane).count : -1;
+            int rank = 0;
+            for (int j = 0; j < a.E; ++j) {
+                const int other = __builtin_amdgcn_readlane(rows, j);
+                rank += other > rows || (other == rows && j < lane) ? 1 : 0;
+            }
+            // the expert of rank l to lane l (lanes past the last expert keep their place)
+            e = __builtin_amdgcn_ds_permute((lane < a.E ? rank : lane) * 4, lane);
+        } else {
+            e = threadIdx.x & 63;
+        }
         for (int e0 = 0; e0 < a.E; e0 += 64) {
             load(e0, total);
             total = __builtin_amdgcn_readlane(incl, 63);
@@ -75,8 +89,7 @@ struct Units {
     }
     __device__ void load(int e0, int before)
     {
-        const int e = e0 + (threadIdx.x & 63);
-        n = e < a.E ? units(group_of(a, e)) : 0;
+        n = e0 + e < a.E ? units(group_of(a, e0 + e)) : 0;
         incl = before + wave_inclusive_sum(n);
     }
     // The expert that unit u belongs to, and its number within the expert.
@@ -88,7 +101,7 @@ struct Units {
             if (m != 0) {
                 const int at = __builtin_ctzll(m);
                 within = u - __builtin_amdgcn_readlane(incl - n, at);
-                return e0 + at;
+                return e0 + __builtin_amdgcn_readlane(e, at);
             }
             before = __builtin_amdgcn_readlane(incl, 63);
         }
@@ -96,8 +109,8 @@ struct Units {
         return -1;
     }
 };
-template <typename F>
-__device__ __forceinline__ Units<F> number_units(const ExpertArgs& a, F f) { return Units<F>(a, f); }
+template <bool SORTED, typename F>
+__device__ __forceinline__ Units<SORTED, F> number_units(const ExpertArgs& a, F f) { return Units<SORTED, F>(a, f); }
 
 // Waits until at most N of the wave's copies to LDS are in flight; the LDS reads
 // that follow stay behind it.
@@ -358,10 +371,10 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
     const int P = KIND == FWD ? a.K : a.C;                     // features of the output
     const int ptiles = (P + TP - 1) / TP, qtiles = KIND == WEIGHT ? (a.K + TQ - 1) / TQ : 1;
     // units of work: row tiles, or (weight) experts and parts of one
-    auto all = number_units(a, [&](const Group& g) {
+    auto all = number_units<KIND == WEIGHT>(a, [&](const Group& g) {
         return KIND == WEIGHT ? (int)max((g.count + a.split_rows - 1) / a.split_rows, (int64_t)1) : (int)((g.count + TQ - 1) / TQ);
     });
-    const int total = all.total * ptiles;                      // (row tiles)
+    const int per = ptiles * qtiles, total = all.total * per;
     auto place = [&](int unit, int pt, int qt) {
         Tile t;
         int within;
@@ -377,28 +390,27 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
         t.len = KIND == WEIGHT ? min((int64_t)a.split_rows, left) : KIND == FWD ? a.C : a.K;
         return t;
     };
-    // The workgroup's `turn`-th tile; e < 0: there is none.
+    // The workgroup's `turn`-th tile; e < 0: there is none.  A turn is a
+    // contiguous range of all tiles, and an XCD's part of it is one as well, so
+    // that tiles that run at one time share operands in the cache.
     auto tile_of = [&](int turn) {
         Tile none;
         none.e = -1;
-        if (KIND == WEIGHT) {
-            // Units of very different lengths: every XCD takes an equal share
-            // of the tiles of each (contiguous, so that they share operands),
-            // the shares turning from unit to unit.
-            const int per = ptiles * qtiles, share = (per + 7) >> 3;
-            const int j = blockIdx.x >> 3, unit = j / share;
-            const int t = (((int)blockIdx.x + unit) & 7) * share + j - unit * share;
-            if (turn > 0 || t >= per) return none;
-            return place(unit, t / qtiles, t % qtiles);
-        }
-        // Blocks of eight row tiles by all feature tiles, so that the tiles
-        // that run at one time share both operands in the cache (four: 2 to
-        // 10% slower at 16384 rows, 2048 -> 8192 features, 8 experts); a turn
-        // is a contiguous range, and an XCD's part of it is one as well.
-        constexpr int GR = 8;
         const int first = turn * (int)gridDim.x, n = min((int)gridDim.x, total - first);
         if ((int)blockIdx.x >= n) return none;
-        const int b = first + xcd_remap(blockIdx.x, n);
+        const int at = xcd_remap(blockIdx.x, n);
+        if (KIND == WEIGHT) {
+            // The units come longest first, and every other turn goes
+            // backwards: who had one of a turn's longer ones has one of the next
+            // turn's shorter ones.
+            const int b = first + (turn & 1 ? n - 1 - at : at);
+            const int unit = b / per, in_unit = b - unit * per;
+            return place(unit, in_unit / qtiles, in_unit % qtiles);
+        }
+        // blocks of eight row tiles by all feature tiles (four: 2 to 10% slower
+        // at 16384 rows, 2048 -> 8192 features, 8 experts)
+        constexpr int GR = 8;
+        const int b = first + at;
         const int blk = b / (GR * ptiles), in_blk = b - blk * GR * ptiles;
         const int h = min(GR, all.total - blk * GR);
         const int pt = in_blk / h;
@@ -511,13 +523,11 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
         }
     };
 
-    const int pw = wp * (TP / NWP), ql = wq * (TQ / NWQ) + (lane & 15);
-    if (KIND == WEIGHT) {
-        start(t);
-        product(t);
+    // A finished tile of the weight gradient, into the gradient or, of a part
+    // of an expert, into its slot of partial sums.
+    auto put_weight = [&](const Tile& t) {
         float* out = nullptr;
-        const int64_t count = group_of(a, t.e).count;
-        if (count > a.split_rows) {
+        if (group_of(a, t.e).count > a.split_rows) {
             // the expert's slots follow those of the split experts before it
             auto slots = [&](const Group& gg) {
                 return gg.count > a.split_rows ? (int)((gg.count + a.split_rows - 1) / a.split_rows) : 0;
@@ -532,41 +542,46 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
             out = static_cast<float*>(a.out) + (int64_t)t.e * a.K * a.C;
         }
         const __amdgpu_buffer_rsrc_t r = make_rsrc(out, out ? (uint32_t)a.K * (uint32_t)a.C * 4u : 0u);
-        const int pl = t.p0 + pw + 4 * (lane >> 4);
+        const int p = t.p0 + wp * (TP / NWP) + 4 * (lane >> 4), q = t.q0 + wq * (TQ / NWQ) + (lane & 15);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int k = t.q0 + ql + j * 16;
+        for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
                 // non-temporal: the gradients are not read again here, and as
                 // ordinary stores they push the operands out of the L2 (64
                 // experts of 512 rows on average, 2048 -> 1408: 385 us, 323 so)
-                const uint32_t off = k < a.K && pl + i * 16 < a.C ? ((uint32_t)k * (uint32_t)a.C + pl + i * 16) * 4u : kOOB;
+                const int k = q + j * 16, c = p + i * 16;
+                const uint32_t off = k < a.K && c < a.C ? ((uint32_t)k * (uint32_t)a.C + c) * 4u : kOOB;
                 __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), r, off, 0, 2);
             }
-        }
-        return;
-    }
+    };
+
     // A workgroup stays for all its tiles: the next one's first copies are
-    // under way while a finished one is stored.  (One tile to a workgroup: 14
-    // us from a tile's last product to the next one's first, of 61 us a tile at
-    // 2048 reduction indices.)
+    // under way while a finished one is stored.
     start(t);
     for (int turn = 1;; ++turn) {
         const Tile next = tile_of(turn);
         product(t);
-        const Out out(a, t.row0, t.qrows);
         uint32_t live[FN];
+        if (KIND == DATA) {
+            const Out out(a, t.row0, t.qrows);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) live[j] = out.load_live(wq * (TQ / NWQ) + j * 16, t.p0 + pw);
+            for (int j = 0; j < FN; ++j) live[j] = out.load_live(wq * (TQ / NWQ) + j * 16, t.p0 + wp * (TP / NWP));
+        }
         if (next.e >= 0) {
             wait_reads();
             barrier();   // every wave is done with both buffers
             start(next);
         }
+        if (KIND == WEIGHT) {
+            put_weight(t);
+        } else {
+            const Out out(a, t.row0, t.qrows);
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-            out.put(lds_out[wave], wq * (TQ / NWQ) + j * 16, t.p0 + pw, [&](int i) { return acc[i][j]; }, live[j]);
+            for (int j = 0; j < FN; ++j)
+                out.put(lds_out[wave], wq * (TQ / NWQ) + j * 16, t.p0 + wp * (TP / NWP), [&](int i) { return acc[i][j]; },
+                        KIND == DATA ? live[j] : 0u);
+        }
         if (next.e < 0) return;
         t = next;
     }
@@ -589,7 +604,7 @@ __global__ __launch_bounds__(NW * 64) void expert_stream_kernel(ExpertArgs a)
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int P = KIND == FWD ? a.K : a.C, ptiles = (P + TP - 1) / TP;
-    auto all = number_units(a, [&](const Group& g) { return (int)((g.count + TQ - 1) / TQ); });
+    auto all = number_units<false>(a, [&](const Group& g) { return (int)((g.count + TQ - 1) / TQ); });
     const int nunits = all.total, total = nunits * ptiles;
     if ((int)blockIdx.x >= total) return;
     // as in the tiled kernel: row tiles of one expert meet in one XCD
@@ -720,12 +735,13 @@ hipError_t launch_tiles(const ExpertArgs& a, hipStream_t s)
 {
     const int P = KIND == FWD ? a.K : a.C;
     const int64_t per = (int64_t)((P + TP - 1) / TP) * (KIND == WEIGHT ? (a.K + TQ - 1) / TQ : 1);
-    const int64_t grid = KIND == WEIGHT ? (a.rows / a.split_rows + a.E) * ((per + 7) / 8 * 8) : most_units(a.rows, a.E, TQ) * per;
+    const int64_t grid = (KIND == WEIGHT ? a.rows / a.split_rows + a.E : most_units(a.rows, a.E, TQ)) * per;
     if (grid == 0) return hipSuccess;
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
-    // as many workgroups as are resident (by their LDS), where they stay for several tiles
-    const int64_t resident = (int64_t)CBW_NUM_CUS * (163840 / ((TP + TQ) * 256 + TP * TQ / (TQ / NWQ / 16) * (int)sizeof(T)));
-    expert_kernel<T, KIND, TP, TQ, NWP, NWQ><<<(int)(KIND == WEIGHT ? grid : std::min(grid, resident)), NWP * NWQ * 64, 0, s>>>(a);
+    // as many workgroups as are resident (by their LDS), which stay for several tiles
+    const int64_t lds = (TP + TQ) * 256 + (KIND == WEIGHT ? 16 : NWQ * TP * 16 * (int)sizeof(T));
+    const int64_t resident = (int64_t)CBW_NUM_CUS * (163840 / lds);
+    expert_kernel<T, KIND, TP, TQ, NWP, NWQ><<<(int)std::min(grid, resident), NWP * NWQ * 64, 0, s>>>(a);
     return hipGetLastError();
 }
 
