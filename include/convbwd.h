@@ -356,7 +356,7 @@ int cbw_set_profile_events(int op, void* start, void* stop);
  * r of expert e, offsets[e] <= r < offsets[e + 1], meets W[e], stored [K][C]
  * with the input features innermost (KRSC).
  *
- *   Y[r,k]    = sum_c X[r,c] W[e,k,c]                (ReLU with CBW_FLAG_RELU)
+ *   Y[r,k]    = sum_c X[r,c] W[e,k,c]                (CBW_FLAG_RELU: non-positive and NaN sums give +0.0)
  *   dX[r,c]   = live[r,c] ? sum_k dY[r,k] W[e,k,c] : +0.0
  *   dW[e,k,c] = sum_{r of e} dY[r,k] X[r,c]          (float32; 0 without rows)
  *

@@ -386,6 +386,8 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
         t.q0 = qt * TQ;
         t.row0 = g.first + (int64_t)t.within * (KIND == WEIGHT ? a.split_rows : TQ);
         const int64_t left = g.first + g.count - t.row0;
+        // (offsets that decrease can count up to anything: no tile outside its group)
+        if (t.within < 0 || left < 0 || (left == 0 && (KIND != WEIGHT || t.within > 0))) t.e = -1;
         t.qrows = KIND == WEIGHT ? 0 : (int)min((int64_t)TQ, left);
         t.len = KIND == WEIGHT ? min((int64_t)a.split_rows, left) : KIND == FWD ? a.C : a.K;
         return t;
@@ -621,6 +623,7 @@ __global__ __launch_bounds__(NW * 64) void expert_stream_kernel(ExpertArgs a)
     const int p0 = pt * TP;
     const int64_t row0 = g.first + (int64_t)within * TQ;
     const int qrows = (int)min((int64_t)TQ, g.first + g.count - row0);
+    if (within < 0 || qrows <= 0) return;   // (offsets that decrease)
     const int64_t qstride = KIND == FWD ? a.x_stride : a.y_stride;
     const int len = KIND == FWD ? a.C : a.K;
     const T* w = static_cast<const T*>(a.p) + (int64_t)e * a.K * a.C;

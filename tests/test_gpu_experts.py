@@ -103,6 +103,68 @@ def test_products(case, dtype):
     ref.check(dW, dw, m, "dW")
 
 
+def _lengths(E, rows, seed):
+    """Uneven group lengths that add up to `rows`, the second group empty."""
+    g = torch.Generator().manual_seed(seed)
+    p = torch.exp(torch.randn(E, generator=g))
+    p[1] = 0.0
+    n = torch.floor(p / p.sum() * rows).long()
+    n[0] += rows - n.sum()
+    return [0] + n.cumsum(0).tolist()
+
+
+# (experts, rows, the output's features, the reduction's, type): sizes at
+# which the large tiles run, several of them to a workgroup, with one, two and
+# more reduction steps and a last one that is short
+LARGE = [
+    (4, 9000, 4128, 64, "bf16"),       # 256 x 256 tiles, one step
+    (4, 9000, 4104, 72, "bf16"),       # two
+    (5, 8000, 4128, 264, "bf16"),      # five
+    (20, 2000, 4104, 200, "bf16"),     # 128 x 128 tiles
+    (3, 2000, 264, 1032, "bf16"),      # few tiles: rows by 64
+    (6, 5001, 1032, 72, "f32"),        # 64 x 64 tiles
+    (100, 3000, 264, 264, "bf16"),     # more experts than lanes
+    (100, 3000, 264, 132, "f32"),
+]
+
+
+@pytest.mark.parametrize("E,rows,P,R,dtype", LARGE)
+def test_large_tiles(E, rows, P, R, dtype):
+    print("[case]", E, rows, P, R, dtype, flush=True)
+    off = _lengths(E, rows, 3)
+    o = torch.tensor(off, dtype=torch.int32, device="cuda")
+    x, w, _, _ = _draw(off, rows, R, P, dtype, 7)
+    d = cb.ExpertDesc.make(E, rows, R, P, dtype)
+    Y = torch.full((rows, P), float("nan"), dtype=DT[dtype], device="cuda")
+    mask = torch.zeros((rows * P + 31) // 32, dtype=torch.int32, device="cuda") if P % 32 == 0 else None
+    cb.expert_fwd(d, x.cuda(), w.cuda(), o, Y, mask, cb.expert_workspace(d), cb.CBW_FLAG_RELU)
+    ref.check(Y, *ref.expert_fwd(x, w, off, True), "Y")
+    if mask is not None:
+        assert torch.equal(mask.cpu(), ref.bits(Y.cpu() > 0)), "footprint"
+    # the data gradient with as many features to write and as many to reduce
+    _, w, dy, live = _draw(off, rows, P, R, dtype, 8)
+    d = cb.ExpertDesc.make(E, rows, P, R, dtype)
+    for lv in (None, live):
+        dX = torch.full((rows, P), float("nan"), dtype=DT[dtype], device="cuda")
+        cb.expert_bwd_data(d, dy.cuda(), w.cuda(), o, None if lv is None else ref.bits(lv).cuda(), dX, cb.expert_workspace(d))
+        ref.check(dX, *ref.expert_bwd_data(dy, w, off, lv), "dX")
+
+
+@pytest.mark.parametrize("E,rows,C,K,dtype", [(5, 2501, 2056, 2056, "bf16"), (3, 9000, 520, 264, "bf16"), (70, 1500, 264, 520, "bf16"),
+                                              (5, 3001, 264, 520, "f32"), (64, 4000, 520, 136, "bf16")])
+def test_large_weight_gradients(E, rows, C, K, dtype):
+    """Several tiles to a workgroup, experts in order of their lengths, split and whole ones side by side."""
+    print("[case]", E, rows, C, K, dtype, flush=True)
+    off = _lengths(E, rows, 4)
+    x, _, dy, _ = _draw(off, rows, C, K, dtype, 9)
+    d = cb.ExpertDesc.make(E, rows, C, K, dtype)
+    ws = cb.expert_workspace(d)
+    ws.fill_(255)
+    dW = torch.full((E, K, C), float("nan"), device="cuda")
+    cb.expert_bwd_weight(d, x.cuda(), dy.cuda(), torch.tensor(off, dtype=torch.int32, device="cuda"), dW, ws)
+    ref.check(dW, *ref.expert_bwd_weight(x, dy, off), "dW")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_split_experts(dtype):
     """Experts whose rows are taken in several parts, between ones that are
