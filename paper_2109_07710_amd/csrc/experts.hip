@@ -239,15 +239,17 @@ struct Operand {
     }
 };
 
-// Output of the forward product and the data gradient: rows of P features,
-// `stride` elements apart, a tile's first row at offset 0.
+// Output rows of P features, `stride` elements apart, a tile's first row at
+// offset 0 (weight gradient: an output feature's row of input features).
 //
 // A wave has 16 rows by 16 I features at a time, a lane four features of each
 // block of 16: stored so, an instruction would write 32 bytes to each of 16
 // rows (bf16).  They pass through the wave's own piece of LDS instead, and a
 // lane takes a vector of consecutive features of one row, with the footprint's
-// bits for them next to each other: an instruction writes whole lines
-// (16384 rows, 2048 -> 8192: 120 us less of 550 spent on stores).
+// bits for them next to each other: an instruction writes whole lines.  (16384
+// rows, 2048 -> 8192: 550 us, 507 so.  Weight gradient of 64 experts, 32768
+// rows, 2048 -> 1408, whose lines would be written by halves: 1.1 GB written
+// for 0.74 GB of results and 402 us, 313 so.)
 template <typename T, int KIND, int I>
 struct Output {
     static constexpr int E = 16 / (int)sizeof(T);              // features of a vector
@@ -265,6 +267,11 @@ struct Output {
         : a(args), row0(first), stride(KIND == FWD ? args.y_stride : args.x_stride), rows(n), P(KIND == FWD ? args.K : args.C)
     {
         r = make_rsrc(static_cast<T*>(a.out) + row0 * stride, (uint32_t)(((rows - 1) * stride + P) * (int64_t)sizeof(T)));
+    }
+    // (weight gradient: n rows of `out`, null: nothing is written)
+    __device__ Output(const ExpertArgs& args, float* out, int n) : a(args), row0(0), stride(args.C), rows(n), P(args.C)
+    {
+        r = make_rsrc(out, out ? (uint32_t)rows * (uint32_t)P * 4u : 0u);
     }
 
     // the row and the feature of the lane's t-th vector, from the block's first
@@ -328,7 +335,11 @@ struct Output {
                     w[k] &= sizeof(T) == 2 ? ((b >> 2 * k) & 1u ? 0xffffu : 0u) | ((b >> (2 * k + 1)) & 1u ? 0xffff0000u : 0u)
                                            : ((b >> k) & 1u ? ~0u : 0u);
             }
-            __builtin_amdgcn_raw_buffer_store_b128(w, r, ok ? (uint32_t)(q * stride + p) * (uint32_t)sizeof(T) : kOOB, 0, 0);
+            // Weight gradients are stored non-temporally: they are not read again
+            // here, and as ordinary stores they push the operands out of the L2
+            // (64 experts of 512 rows on average, 2048 -> 1408: 333 us, 313 so).
+            __builtin_amdgcn_raw_buffer_store_b128(w, r, ok ? (uint32_t)(q * stride + p) * (uint32_t)sizeof(T) : kOOB, 0,
+                                                   KIND == WEIGHT ? 2 : 0);
             if (KIND == FWD && a.out_mask) {
                 // (after ReLU a stored value is positive unless its bits are zero)
                 uint32_t b = 0;
@@ -356,7 +367,9 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
     __shared__ __align__(1024) char lds_p[2][OP::BYTES];
     __shared__ __align__(1024) char lds_q[2][OQ::BYTES];
     using Out = Output<T, KIND, FM>;
-    __shared__ __align__(1024) char lds_out[KIND == WEIGHT ? 1 : NW][KIND == WEIGHT ? 16 : Out::BYTES];
+    constexpr int WI = FM < 4 ? FM : 4;   // blocks of the weight gradient to a row in LDS
+    using OutW = Output<float, KIND, WI>;
+    __shared__ __align__(1024) char lds_out[NW][KIND == WEIGHT ? OutW::BYTES : Out::BYTES];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wp = wave / NWQ, wq = wave % NWQ;
@@ -543,19 +556,13 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void expert_kernel(ExpertArgs a)
         } else {
             out = static_cast<float*>(a.out) + (int64_t)t.e * a.K * a.C;
         }
-        const __amdgpu_buffer_rsrc_t r = make_rsrc(out, out ? (uint32_t)a.K * (uint32_t)a.C * 4u : 0u);
-        const int p = t.p0 + wp * (TP / NWP) + 4 * (lane >> 4), q = t.q0 + wq * (TQ / NWQ) + (lane & 15);
+        const OutW rows(a, out ? out + (int64_t)t.q0 * a.C : nullptr, min(TQ, a.K - t.q0));
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                // non-temporal: the gradients are not read again here, and as
-                // ordinary stores they push the operands out of the L2 (64
-                // experts of 512 rows on average, 2048 -> 1408: 385 us, 323 so)
-                const int k = q + j * 16, c = p + i * 16;
-                const uint32_t off = k < a.K && c < a.C ? ((uint32_t)k * (uint32_t)a.C + c) * 4u : kOOB;
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), r, off, 0, 2);
-            }
+            for (int h = 0; h < FM; h += WI)
+                rows.put(lds_out[wave], wq * (TQ / NWQ) + j * 16, t.p0 + wp * (TP / NWP) + h * 16,
+                         [&](int i) { return acc[h + i][j]; }, 0u);
     };
 
     // A workgroup stays for all its tiles: the next one's first copies are
@@ -742,7 +749,7 @@ hipError_t launch_tiles(const ExpertArgs& a, hipStream_t s)
     if (grid == 0) return hipSuccess;
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
     // as many workgroups as are resident (by their LDS), which stay for several tiles
-    const int64_t lds = (TP + TQ) * 256 + (KIND == WEIGHT ? 16 : NWQ * TP * 16 * (int)sizeof(T));
+    const int64_t lds = (TP + TQ) * 256 + (KIND == WEIGHT ? NWP * NWQ * std::min(64, TP / NWP) * 64 : NWQ * TP * 16 * (int)sizeof(T));
     const int64_t resident = (int64_t)CBW_NUM_CUS * (163840 / lds);
     expert_kernel<T, KIND, TP, TQ, NWP, NWQ><<<(int)std::min(grid, resident), NWP * NWQ * 64, 0, s>>>(a);
     return hipGetLastError();
