@@ -245,7 +245,7 @@ int expert_bwd_weight(const cbw_expert_desc* desc, const void* X, const void* dY
     a.partial = static_cast<float*>(workspace);
     a.split_rows = plan.split_rows;
     a.slots = plan.slots;
-    return hip_status(launch_expert_bwd_weight(desc->dtype, a, static_cast<hipStream_t>(stream)));
+    return hip_status(launch_expert_bwd_weight(desc->dtype, a, plan.large, static_cast<hipStream_t>(stream)));
 }
 
 int cbw_validate_norm_desc(const cbw_norm_desc* d)

@@ -103,6 +103,7 @@ struct ExpertArgs {
 // workgroups of its own.  An expert with more than one part has a slot of
 // partial sums for each: fewer than 2 rows / split_rows slots in all.
 struct ExpertPlan {
+    bool large;                 // tiles of 256 x 256
     int split_rows;
     int64_t slots;
     size_t ws_bytes;
@@ -111,7 +112,7 @@ ExpertPlan expert_plan(const cbw_expert_desc* d);
 
 hipError_t launch_expert_fwd(int dtype, const ExpertArgs& a, hipStream_t s);
 hipError_t launch_expert_bwd_data(int dtype, const ExpertArgs& a, hipStream_t s);
-hipError_t launch_expert_bwd_weight(int dtype, const ExpertArgs& a, hipStream_t s);
+hipError_t launch_expert_bwd_weight(int dtype, const ExpertArgs& a, bool large, hipStream_t s);
 
 // ------------------------------------------------------- gradient clipping
 

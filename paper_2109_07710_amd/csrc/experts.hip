@@ -803,15 +803,34 @@ hipError_t launch_rows(const ExpertArgs& a, hipStream_t s)
 
 }  // namespace
 
-// Parts long enough that their sums' way through memory stays small beside
-// the products, and short enough that there are about two tiles for a CU.
+// Weight gradient: tiles and parts.
+//
+// bf16, large tiles where an expert's rows make the product outweigh a tile's
+// start and end and there is one for every CU (us, 256 x 256 | 128 x 128: 512
+// rows for each of 64 experts, 2048 -> 1408: 294 | 345; 4 of 1024, 2048 ->
+// 2048: 41 | 51; 25 of 92, 2048 -> 4096: 175 | 160; 8 of 2048, 1024 -> 1024: 50
+// | 44).
+//
+// Splitting an expert's rows sends every part's sums through memory and back,
+// the products' own time for parts of about 1000 rows (bf16).  So they are
+// split where the experts' tiles leave half the chip idle or more, into parts
+// that fill it (16384 rows, 1 expert, 1024 -> 1024: 192 us whole, 52 by 2048
+// rows, 61 by 1024); and otherwise only an expert that is three times the mean
+// and would alone take half the call's time (the uneven 64 experts, longest
+// 5591: 376 us whole, 317 by 3072 rows; 8 even ones of 2048 rows, 1024 -> 1024:
+// 44 whole, 73 by 2048).
 ExpertPlan expert_plan(const cbw_expert_desc* d)
 {
     ExpertPlan p{};
-    const int side = d->dtype == CBW_F32 ? 64 : 256;
-    const int64_t tiles = (int64_t)((d->C + side - 1) / side) * ((d->K + side - 1) / side);
-    const int64_t len = std::max<int64_t>(512, (d->rows * tiles / 512 + 63) / 64 * 64);
-    p.split_rows = (int)std::min<int64_t>(len, 1 << 30);
+    const bool f32 = d->dtype == CBW_F32;
+    const int64_t busy = std::max<int64_t>(1, std::min<int64_t>(d->E, d->rows)), mean = (d->rows + busy - 1) / busy;
+    auto tiles = [&](int side) { return (int64_t)((d->C + side - 1) / side) * ((d->K + side - 1) / side); };
+    p.large = !f32 && mean >= 256 && tiles(256) * busy >= CBW_NUM_CUS;
+    const int64_t per = tiles(f32 ? 64 : p.large ? 256 : 128), resident = CBW_NUM_CUS * (f32 ? 4 : p.large ? 1 : 2);
+    const int64_t share = d->rows * per / resident;   // rows of one tile that a workgroup takes on average
+    int64_t len = std::max(3 * mean, share / 2);
+    if (2 * per * busy <= resident) len = std::max<int64_t>(f32 ? 256 : 1024, share);
+    p.split_rows = (int)std::min<int64_t>((std::max<int64_t>(len, 256) + 63) / 64 * 64, 1 << 30);
     p.slots = d->rows > p.split_rows ? 2 * d->rows / p.split_rows : 0;
     p.ws_bytes = (size_t)p.slots * d->K * d->C * 4;
     return p;
@@ -827,17 +846,11 @@ hipError_t launch_expert_bwd_data(int dtype, const ExpertArgs& a, hipStream_t s)
     return dtype == CBW_F32 ? launch_rows<float, DATA>(a, s) : launch_rows<uint16_t, DATA>(a, s);
 }
 
-// Weight gradient, bf16: large tiles where an expert's rows make the product
-// outweigh a tile's start and end (us, 256 x 256 | 128 x 128: 1024 rows for
-// each of 64 experts, 2048 -> 1408: 490 | 592; 512 on average: 323 | 338; 36
-// experts of 193, 1736 -> 1312: 205 | 190; 47 of 4, 816 -> 280: 22 | 17).
-hipError_t launch_expert_bwd_weight(int dtype, const ExpertArgs& a, hipStream_t s)
+hipError_t launch_expert_bwd_weight(int dtype, const ExpertArgs& a, bool large, hipStream_t s)
 {
-    const int64_t mean = std::min<int64_t>(a.rows / std::max<int64_t>(1, std::min<int64_t>(a.E, a.rows)), a.split_rows);
-    const int64_t tiles = (int64_t)((a.C + 255) / 256) * ((a.K + 255) / 256) * (a.rows / a.split_rows + a.E);
     hipError_t e;
     if (dtype == CBW_F32) e = launch_tiles<float, WEIGHT, 64, 64, 2, 2>(a, s);
-    else if (mean >= 400 && tiles >= 256) e = launch_tiles<uint16_t, WEIGHT, 256, 256, 2, 4>(a, s);
+    else if (large) e = launch_tiles<uint16_t, WEIGHT, 256, 256, 2, 4>(a, s);
     else e = launch_tiles<uint16_t, WEIGHT, 128, 128, 2, 2>(a, s);
     if (e != hipSuccess || a.rows <= a.split_rows) return e;
     expert_sum_kernel<<<1024, 256, 0, s>>>(a);
