@@ -711,29 +711,42 @@ __global__ __launch_bounds__(NW * 64) void expert_stream_kernel(ExpertArgs a)
     }
 }
 
-// Sums of the split experts' parts, in order.
+// Sums of the split experts' parts, in order.  Pieces of 256 vectors of all
+// split experts are dealt out to the workgroups.
 __global__ __launch_bounds__(256) void expert_sum_kernel(ExpertArgs a)
 {
-    const int64_t vecs = (int64_t)a.K * a.C / 4;
-    int64_t slot = 0;
+    const int64_t vecs = (int64_t)a.K * a.C / 4, pieces = (vecs + 255) / 256;
+    int64_t slot0 = 0, piece = blockIdx.x;   // slots of the experts before; the next piece, from this group of experts on
     for (int e0 = 0; e0 < a.E; e0 += 64) {
         const int x = e0 + (threadIdx.x & 63);
-        int n = 0;
-        if (x < a.E) n = (int)((group_of(a, x).count + a.split_rows - 1) / a.split_rows);
-        uint64_t todo = __ballot(n > 1);
-        for (; todo != 0; todo &= todo - 1) {
-            const int at = __builtin_ctzll(todo);
-            const int parts = __builtin_amdgcn_readlane(n, at);
-            if (slot + parts > a.slots) return;   // (offsets that decrease)
+        const int n = x < a.E ? (int)((group_of(a, x).count + a.split_rows - 1) / a.split_rows) : 0;
+        const int parts = n > 1 ? n : 0, last = wave_inclusive_sum(parts);
+        const uint64_t split = __ballot(parts > 0);
+        const int before = __popcll(split & ((1ull << (threadIdx.x & 63)) - 1));   // split experts before the lane's
+        const int64_t mine = __popcll(split) * pieces;
+        for (; piece < mine; piece += gridDim.x) {
+            const int64_t rank = piece / pieces;
+            const int at = __builtin_ctzll(__ballot(parts > 0 && before == (int)rank));
+            const int np = __builtin_amdgcn_readlane(parts, at);
+            const int64_t slot = slot0 + __builtin_amdgcn_readlane(last, at) - np;
+            const int64_t i = (piece - rank * pieces) * 256 + threadIdx.x;
+            if (slot + np > a.slots) return;   // (offsets that decrease)
+            if (i >= vecs) continue;
             const floatx4* src = reinterpret_cast<const floatx4*>(a.partial) + slot * vecs;
-            floatx4* dst = reinterpret_cast<floatx4*>(static_cast<float*>(a.out)) + (int64_t)(e0 + at) * vecs;
-            for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < vecs; i += (int64_t)gridDim.x * 256) {
-                floatx4 s = src[i];
-                for (int z = 1; z < parts; ++z) s += src[z * vecs + i];
-                dst[i] = s;
+            // eight loads in flight, added in order
+            floatx4 s = {};
+            for (int z = 0; z < np; z += 8) {
+                floatx4 v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = src[(int64_t)min(z + k, np - 1) * vecs + i];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (z + k < np) s += v[k];
             }
-            slot += parts;
+            reinterpret_cast<floatx4*>(static_cast<float*>(a.out))[(e0 + at) * vecs + i] = s;
         }
+        piece -= mine;
+        slot0 += __builtin_amdgcn_readlane(last, 63);
     }
 }
 
@@ -813,9 +826,10 @@ hipError_t launch_rows(const ExpertArgs& a, hipStream_t s)
 //
 // Splitting an expert's rows sends every part's sums through memory and back,
 // the products' own time for parts of about 1000 rows (bf16).  So they are
-// split where the experts' tiles leave half the chip idle or more, into parts
-// that fill it (16384 rows, 1 expert, 1024 -> 1024: 192 us whole, 52 by 2048
-// rows, 61 by 1024); and otherwise only an expert that is three times the mean
+// split where the experts' tiles leave half the chip idle or more, into three
+// parts or more that fill it (16384 rows, 1 expert, 1024 -> 1024: 186 us whole,
+// 52 by 2048 rows, 62 by 1024; 1531 rows, 792 -> 3432: 27 whole, 37 by 512);
+// and otherwise only an expert that is three times the mean
 // and would alone take half the call's time (the uneven 64 experts, longest
 // 5591: 376 us whole, 317 by 3072 rows; 8 even ones of 2048 rows, 1024 -> 1024:
 // 44 whole, 73 by 2048).
@@ -829,7 +843,9 @@ ExpertPlan expert_plan(const cbw_expert_desc* d)
     const int64_t per = tiles(f32 ? 64 : p.large ? 256 : 128), resident = CBW_NUM_CUS * (f32 ? 4 : p.large ? 1 : 2);
     const int64_t share = d->rows * per / resident;   // rows of one tile that a workgroup takes on average
     int64_t len = std::max(3 * mean, share / 2);
-    if (2 * per * busy <= resident) len = std::max<int64_t>(f32 ? 256 : 1024, share);
+    // (small filters' sums are soon moved: 26 experts of 1683 rows, 56 -> 248, 26 us whole, 17 by 512 rows, 22 by 1024)
+    const int64_t filling = std::max<int64_t>((int64_t)d->K * d->C <= 1 << 18 ? 512 : 1024, share);
+    if (2 * per * busy <= resident && mean >= 3 * filling) len = filling;
     p.split_rows = (int)std::min<int64_t>((std::max<int64_t>(len, 256) + 63) / 64 * 64, 1 << 30);
     p.slots = d->rows > p.split_rows ? 2 * d->rows / p.split_rows : 0;
     p.ws_bytes = (size_t)p.slots * d->K * d->C * 4;
