@@ -16,9 +16,16 @@
 // element by element (float32, whose matrix instruction takes one reduction
 // index a lane).
 //
-// Every workgroup finds its expert and tile itself: a wave scans the group
+// Every workgroup finds its experts and tiles itself: a wave scans the group
 // lengths (E + 1 offsets, in the cache) and looks its own number up.  The
 // grid covers the most tiles any lengths can give; surplus workgroups leave.
+//
+// Bound by the matrix cores where an expert has some hundred rows (16384 rows
+// over 8 experts, 2048 -> 8192 features, bf16: 503 us, 1090 TFLOP/s; with groups
+// of whole tiles 475 us, 1155), by reading the filters where it has few (12
+// rows over 32 experts, 2048 -> 1408: 10.7 us, 5.5 TB/s), and the weight
+// gradient of narrow experts by writing it (64 experts, 32768 rows: 310 us,
+// 3.1 TB/s beside 610 TFLOP/s).
 #include "common.hpp"
 #include "block_kernels.hpp"
 #include "tiles.hpp"
@@ -842,11 +849,12 @@ ExpertPlan expert_plan(const cbw_expert_desc* d)
     p.large = !f32 && mean >= 256 && tiles(256) * busy >= CBW_NUM_CUS;
     const int64_t per = tiles(f32 ? 64 : p.large ? 256 : 128), resident = CBW_NUM_CUS * (f32 ? 4 : p.large ? 1 : 2);
     const int64_t share = d->rows * per / resident;   // rows of one tile that a workgroup takes on average
-    int64_t len = std::max(3 * mean, share / 2);
+    // (1024 rows of one tile take some 10 us: no more than the launch that adds parts up costs)
+    int64_t len = std::max<int64_t>(1024, std::max(3 * mean, share / 2));
     // (small filters' sums are soon moved: 26 experts of 1683 rows, 56 -> 248, 26 us whole, 17 by 512 rows, 22 by 1024)
     const int64_t filling = std::max<int64_t>((int64_t)d->K * d->C <= 1 << 18 ? 512 : 1024, share);
     if (2 * per * busy <= resident && mean >= 3 * filling) len = filling;
-    p.split_rows = (int)std::min<int64_t>((std::max<int64_t>(len, 256) + 63) / 64 * 64, 1 << 30);
+    p.split_rows = (int)std::min<int64_t>((len + 63) / 64 * 64, 1 << 30);
     p.slots = d->rows > p.split_rows ? 2 * d->rows / p.split_rows : 0;
     p.ws_bytes = (size_t)p.slots * d->K * d->C * 4;
     return p;
