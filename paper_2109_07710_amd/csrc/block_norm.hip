@@ -12,7 +12,7 @@
 // Bound by memory: a row is read once into registers, where its statistics,
 // both norms and every gradient are computed, and written once (16384 rows of
 // 4096, bf16, RMS norms, a gate of its own for each value: forward 135 us, 4.95
-// TB/s, backward 243 us, 4.4 TB/s; 100352 rows of 256, layer norms, float32
+// TB/s, backward 244 us, 4.4 TB/s; 100352 rows of 256, layer norms, float32
 // stream, one gate row for 3136: backward 109 us, 4.25 TB/s).  One vector of 8
 // columns a thread: with two, half as many waves hid less of the loads'
 // latency (backward 374 us).  Statistics

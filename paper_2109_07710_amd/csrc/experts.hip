@@ -21,11 +21,12 @@
 // grid covers the most tiles any lengths can give; surplus workgroups leave.
 //
 // Bound by the matrix cores where an expert has some hundred rows (16384 rows
-// over 8 experts, 2048 -> 8192 features, bf16: 503 us, 1090 TFLOP/s; with groups
+// over 8 experts, 2048 -> 8192 features, bf16: 502 us, 1095 TFLOP/s; with groups
 // of whole tiles 475 us, 1155), by reading the filters where it has few (12
-// rows over 32 experts, 2048 -> 1408: 10.7 us, 5.5 TB/s), and the weight
-// gradient of narrow experts by writing it (64 experts, 32768 rows: 310 us,
-// 3.1 TB/s beside 610 TFLOP/s).
+// rows over 32 experts, 2048 -> 1408: 14.6 us, 4.0 TB/s, filters read from memory;
+// 10.5 to 13 where calls in turn leave part of them in the 256 MB cache).  The weight gradient of narrow experts takes its products and
+// the writing of its results in turn (64 uneven experts, 32768 rows, 2048 ->
+// 1408: 310 to 334 us, 3.1 to 2.9 TB/s beside 610 to 565 TFLOP/s).
 #include "common.hpp"
 #include "block_kernels.hpp"
 #include "tiles.hpp"
@@ -798,12 +799,15 @@ int64_t likely_tiles(const ExpertArgs& a, int tile, int P, int width)
 // the caches but rows enough to fill them and tiles enough to fill the chip;
 // where there are neither, the streaming kernel splits the reduction over its
 // waves.  Measured (us, bf16, forward; 256 x 256 | 128 x 128 | stream, 16 rows |
-// stream, 64 rows): 16384 rows, 8 experts, 2048 -> 8192: 536 | 700 | - | -;
-// 6935 rows, 36 experts, 1736 -> 1312: 56 | 68 | 145 | 107; 3676, 3, 264 ->
-// 1576: 17 | 13 | 37 | 28; 256, 8, 2048 -> 8192: 54 | 44 | 53 | 55; 755, 1, 2664
-// -> 536: 59 | 38 | 14 | 13; 2108, 46, 848 -> 152: 22 | 13 | 7 | 8; 12, 32, 2048
-// -> 1408: 43 | 24 | 12 | 13.  Few tiles of 64 features: 16 rows, 1 expert, 8192
-// -> 512: 17, and 10 with 32 features and eight waves.
+// stream, 64 rows): 16384 rows, 8 experts, 2048 -> 8192: 511 | 653 | - | -;
+// 6935 rows, 36 experts, 1736 -> 1312: 52 | 69 | 141 | 105; 3676, 3, 264 ->
+// 1576: 14 | 12 | 37 | 26; 256, 8, 2048 -> 8192: 52 | 45 | 52 | 54; 755, 1, 2664
+// -> 536: 57 | 38 | 14 | 13; 2108, 46, 848 -> 152: 22 | 14 | 7 | 7; 12, 32, 2048
+// -> 1408: 43 | 26 | 12 | 13.  Few tiles of 64 features: 16 rows, 1 expert, 8192
+// -> 512: 18, and 10 with 32 features and eight waves.  (The small ones' filters
+// lay in the caches.  From memory, 64 features and four waves | 32 and eight:
+// 12 rows, 32 experts, 2048 -> 1408: 15.7 | 16.9; 300, 64, 1024 -> 512: 15 | 22;
+// 1, 1, 2048 -> 8192: 10.3 | 9.5.)
 template <typename T, int KIND>
 hipError_t launch_rows(const ExpertArgs& a, hipStream_t s)
 {
@@ -827,19 +831,20 @@ hipError_t launch_rows(const ExpertArgs& a, hipStream_t s)
 //
 // bf16, large tiles where an expert's rows make the product outweigh a tile's
 // start and end and there is one for every CU (us, 256 x 256 | 128 x 128: 512
-// rows for each of 64 experts, 2048 -> 1408: 294 | 345; 4 of 1024, 2048 ->
-// 2048: 41 | 51; 25 of 92, 2048 -> 4096: 175 | 160; 8 of 2048, 1024 -> 1024: 50
+// rows for each of 64 experts, 2048 -> 1408: 242 | 308; 4 of 1024, 2048 ->
+// 2048: 42 | 51; 25 of 92, 2048 -> 4096: 181 | 158; 8 of 2048, 1024 -> 1024: 51
 // | 44).
 //
 // Splitting an expert's rows sends every part's sums through memory and back,
 // the products' own time for parts of about 1000 rows (bf16).  So they are
 // split where the experts' tiles leave half the chip idle or more, into three
-// parts or more that fill it (16384 rows, 1 expert, 1024 -> 1024: 186 us whole,
-// 52 by 2048 rows, 62 by 1024; 1531 rows, 792 -> 3432: 27 whole, 37 by 512);
+// parts or more that fill it (16384 rows, 1 expert, 1024 -> 1024: 190 us whole,
+// 52 by 2048 rows, 63 by 1024; 1531 rows, 792 -> 3432: 26 whole, 35 by 512);
 // and otherwise only an expert that is three times the mean
-// and would alone take half the call's time (the uneven 64 experts, longest
-// 5591: 376 us whole, 317 by 3072 rows; 8 even ones of 2048 rows, 1024 -> 1024:
-// 44 whole, 73 by 2048).
+// and would alone take half the call's time (64 uneven experts, 32768 rows,
+// 2048 -> 1408, the longest 5591: 377 us whole, 332 in the parts of half a
+// workgroup's share that follow; 8 even ones of 2048 rows, 1024 -> 1024: 44
+// whole, 73 by 1024).
 ExpertPlan expert_plan(const cbw_expert_desc* d)
 {
     ExpertPlan p{};

@@ -12,7 +12,7 @@
 // each add all partials in the same order (8 KB from the L2, under their
 // first chunk's loads) instead of waiting for a launch in between.  A call is
 // two launches, one more for every 120 tensors past the first.  (13 tensors,
-// 59 MB: 32 us; 300 packed ones, 90 MB: 67; 48 of 2.1 GB together: 1280, 5.05
+// 59 MB: 32 us; 300 packed ones, 90 MB: 67; 48 of 2.1 GB together: 1276, 5.05
 // TB/s.)
 #include "common.hpp"
 #include "block_kernels.hpp"
