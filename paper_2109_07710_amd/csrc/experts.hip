@@ -623,10 +623,11 @@ __global__ __launch_bounds__(NW * 64) void expert_stream_kernel(ExpertArgs a)
     const int P = KIND == FWD ? a.K : a.C, ptiles = (P + TP - 1) / TP;
     auto all = number_units<false>(a, [&](const Group& g) { return (int)((g.count + TQ - 1) / TQ); });
     const int nunits = all.total, total = nunits * ptiles;
-    if ((int)blockIdx.x >= total) return;
+    const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;   // (launches of many have a second axis)
+    if (wg >= total) return;
     // as in the tiled kernel: row tiles of one expert meet in one XCD
     constexpr int GR = 8;
-    const int b = xcd_remap(blockIdx.x, total);
+    const int b = xcd_remap((int)wg, total);
     const int blk = b / (GR * ptiles), in_blk = b - blk * GR * ptiles;
     const int h = min(GR, nunits - blk * GR);
     const int pt = in_blk / h;
@@ -783,7 +784,10 @@ hipError_t launch_stream(const ExpertArgs& a, hipStream_t s)
     const int64_t grid = most_units(a.rows, a.E, 16 * FN) * ((P + TP - 1) / TP);
     if (grid == 0) return hipSuccess;
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
-    expert_stream_kernel<T, KIND, TP, FN, NW, RING><<<(int)grid, NW * 64, 0, s>>>(a);
+    // An axis of a launch takes 2^32 - 1 threads; more wrap without an error.
+    const int64_t x = std::min<int64_t>(grid, 1 << 22);
+    static_assert(NW * 64 <= 1 << 9, "threads along the first axis");
+    expert_stream_kernel<T, KIND, TP, FN, NW, RING><<<dim3((unsigned)x, (unsigned)((grid + x - 1) / x)), NW * 64, 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -338,3 +338,27 @@ def test_binding_refuses():
     with pytest.raises(cb.CbwError) as e:
         cb.expert_bwd_weight(big, t(64), t(32), o, torch.zeros((2, 32, 64), device="cuda"), ws[:0])
     assert e.value.status == cb.CBW_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("product", ["forward", "data"])
+def test_more_workgroups_than_one_axis_takes(product):
+    """A row for each of 1024 experts, by so many features that over 2^24
+    workgroups of 256 threads are launched: 2^32 threads, more than a launch
+    has along one axis."""
+    P, R, E = (1 << 20) - 8, 8, 1024
+    o = torch.arange(E + 1, dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(13)
+    x = torch.randn((E, R), generator=g, device="cuda").bfloat16()
+    fwd = product == "forward"
+    w = torch.empty((E, P, R) if fwd else (E, R, P), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    out = torch.full((E, P), float("nan"), dtype=torch.bfloat16, device="cuda")
+    if fwd:
+        d = cb.ExpertDesc.make(E, E, R, P)
+        cb.expert_fwd(d, x, w, o, out, None, cb.expert_workspace(d))
+    else:
+        d = cb.ExpertDesc.make(E, E, P, R)
+        cb.expert_bwd_data(d, x, w, o, None, out, cb.expert_workspace(d))
+    assert not any(bool(v.isnan().any()) for v in out.split(64)), "values were not written"
+    for e in (0, 63, 64, 500, 1023):
+        we, xe = (w[e].t() if fwd else w[e]).cpu().double(), x[e:e + 1].cpu().double()
+        ref.check(out[e:e + 1], xe @ we, (R + 4) * ref.U32 * (xe.abs() @ we.abs()), "expert %d" % e)
