@@ -494,10 +494,10 @@ int grad_norm(const cbw_grad* grads, int32_t n, int32_t kind, float* norm, void*
               void* stream);
 
 /* out = grad * c with c = min(1, max_norm / (norm + 1e-6)); norm (device
- * float32[2]) receives the norm and c.  Nothing is read back: a norm that is
- * infinite gives c = 0 and one that is NaN c = NaN, and the caller who wants
- * to leave out such a step tests norm[0].  A tensor in place (out == grad) is
- * not touched when c is 1.  max_norm is not negative. */
+ * float32[2]) receives the norm and c.  Nothing is read back: where norm[0] is
+ * infinity c is 0, whatever max_norm is, where it is NaN so is c, and the
+ * caller who wants to leave out such a step tests norm[0].  A tensor in place
+ * (out == grad) is not touched when c is 1.  max_norm is not negative. */
 int grad_clip(const cbw_grad* grads, int32_t n, int32_t kind, float max_norm, float* norm, void* workspace,
               size_t workspace_bytes, void* stream);
 

@@ -199,7 +199,9 @@ __global__ __launch_bounds__(GT) void grad_scale_kernel(const GradEntry* table, 
         next.load(table[k], range.end - 1);
     }
     const double total = norm_of<R>(partial, npartial);
-    const double q = (double)max_norm / (total + 1e-6);
+    // A norm that is reported as infinity scales to zero, also where only
+    // float32 cannot hold it and where the limit is infinite as well.
+    const double q = isinf((float)total) ? 0.0 : (double)max_norm / (total + 1e-6);
     const float coef = q >= 1.0 ? 1.0f : (float)q;   // (a NaN stays one)
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         norm[0] = (float)total;

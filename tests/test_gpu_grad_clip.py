@@ -181,3 +181,31 @@ def test_binding_refuses():
     with pytest.raises(cb.CbwError) as e:
         cb.grad_clip(lst, 1.0, norm, ws[:8])
     assert e.value.status == cb.CBW_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("max_norm", [1.0, 1e10, 3e38, math.inf])
+def test_norm_past_float32(dtype, max_norm):
+    """Finite gradients whose 2-norm no float32 holds: the norm is infinity and
+    c is 0, as for an infinite gradient, whatever the limit is."""
+    g = [torch.full((n,), 3e38, device="cuda").to(dtype) for n in (4096, 5)]
+    lst = cb.GradList(g, [torch.full_like(v, 7.0) for v in g])
+    norm, ws = torch.full((2,), 7.0, device="cuda"), cb.grad_workspace(lst)
+    cb.grad_clip(lst, max_norm, norm, ws)
+    assert norm.tolist() == [math.inf, 0.0]
+    assert all((o == 0).all() for o in lst.outs)
+    # and the largest magnitude, which float32 holds, is a norm like any other
+    cb.grad_clip(lst, 1.0, norm, ws, "inf")
+    assert 0 < float(norm[1]) and float(norm[0]) == float(g[0][0])
+
+
+@pytest.mark.parametrize("kind", ["2", "inf"])
+def test_infinite_norm_without_a_limit(kind):
+    """An infinite gradient gives c = 0 where the limit is infinite as well."""
+    g = [torch.ones(3000, device="cuda") for _ in range(2)]
+    g[1][7] = -math.inf
+    lst = cb.GradList(g)
+    norm, ws = torch.full((2,), 7.0, device="cuda"), cb.grad_workspace(lst)
+    cb.grad_clip(lst, math.inf, norm, ws, kind)
+    assert norm.tolist() == [math.inf, 0.0]
+    assert (g[0] == 0).all() and torch.isnan(g[1][7]) and (g[1][8:] == 0).all()
