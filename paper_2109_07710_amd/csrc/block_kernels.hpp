@@ -121,7 +121,7 @@ constexpr int kGradChunk = 16384;     // bytes a workgroup takes at a time
 constexpr int kGradMaxWgs = 1024;     // workgroups of a pass, shared out over its launches,
 constexpr int kGradMinWgs = 256;      // of which each has this many if it has the chunks
 
-struct GradEntry {
+struct alignas(16) GradEntry {   // (copied by 16-byte vectors)
     const void* src;
     void* dst;
     int64_t bytes;              // bit 63: bf16

@@ -114,7 +114,7 @@ __global__ __launch_bounds__(GT) void grad_norm_kernel(GradTable t, double* part
     __shared__ GradEntry e_s[kGradTable];
     const int lane = threadIdx.x & 63;
     const ChunkRange range = my_chunks(t.chunks);
-    static_assert(2 * kGradTable <= GT && sizeof(GradEntry) == 32, "a 16-byte half entry a thread");
+    static_assert(2 * kGradTable <= GT && sizeof(GradEntry) == 32 && alignof(GradEntry) == 16, "an aligned 16-byte half entry a thread");
     if ((int)threadIdx.x < 2 * kGradTable)
         reinterpret_cast<u32x4*>(e_s)[threadIdx.x] = reinterpret_cast<const u32x4*>(t.e)[threadIdx.x];
     __syncthreads();
