@@ -131,6 +131,14 @@ __device__ __forceinline__ void wait_copies()
 // Until the wave's LDS reads have returned: what they read may be overwritten.
 __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
+// Between LDS accesses by which the lanes of one wave exchange values: the
+// LDS serves a wave's in their order, the compiler has to leave them in it.
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint2 lds_read_transposed(const void* lds)
@@ -317,6 +325,7 @@ struct Output {
     __device__ __forceinline__ void put(char* lds, int q0, int p0, const V& v, uint32_t live) const
     {
         const int lane = my_lane(), row = lane & 15;
+        wave_fence();   // (the block before this one has been read)
         // (a row's chunks are moved by its number: the 16 rows' do not share banks)
         auto at = [&](int rr, int chunk) { return lds + rr * ROW + ((chunk ^ (rr & (CHUNKS - 1))) << 4); };
 #pragma unroll
@@ -331,6 +340,7 @@ struct Output {
             else
                 *reinterpret_cast<u32x4*>(at(row, i * 4 + (lane >> 4))) = __builtin_bit_cast(u32x4, x);
         }
+        wave_fence();
 #pragma unroll
         for (int t = 0; t < VECS; ++t) {
             const int rr = row_of(lane, t), q = q0 + rr, p = p0 + feature_of(lane);
