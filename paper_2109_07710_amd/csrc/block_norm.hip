@@ -159,10 +159,22 @@ struct Team {
     }
 };
 
-// The gate's activation and its derivative.
-__device__ __forceinline__ float gate_value(float g, int act)
+// The gate's activation a and its derivative da.  The sigmoid's from e =
+// exp(-|g|), a = 1 / (1 + e) or e / (1 + e), da = e / (1 + e)^2: a (1 - a)
+// would lose the derivative where a is near 1, exp(-g) the value past 88.  For
+// bf16 gates the fast exponential and reciprocal (|g| 2^-23 and 2^-23 relative,
+// nothing beside the outputs' 2^-9) with the fewer registers.
+struct Gate {
+    float a, da;
+};
+template <typename TB>
+__device__ __forceinline__ Gate gate_at(float g, int act)
 {
-    return act == CBW_GATE_SIGMOID ? 1.f / (1.f + __expf(-g)) : g;
+    if (act != CBW_GATE_SIGMOID) return {g, 1.f};
+    const bool exact = sizeof(TB) == 4;
+    const float e = exact ? expf(-fabsf(g)) : __expf(-fabsf(g));
+    const float r = exact ? 1.f / (1.f + e) : __builtin_amdgcn_rcpf(1.f + e), er = e * r;
+    return {g < 0.f ? er : r, er * r};
 }
 
 // Mean and reciprocal deviation of the row v (columns past C hold zeros).
@@ -255,7 +267,7 @@ __global__ __launch_bounds__(WT ? WT : 256) void norm_fwd_kernel(NormArgs a, int
                     // (columns past C stay zeros)
                     const float n = a.post == CBW_NORM_NONE ? u[i].f[j] : in[i] ? (u[i].f[j] - mu_u) * r_u : 0.f;
                     const float z = fmaf(n, w.f[j], b.f[j]) * s.f[j];
-                    y[i].f[j] = fmaf(z, a.gate ? gate_value(g[i].f[j], a.act) : 1.f, y[i].f[j]);
+                    y[i].f[j] = fmaf(z, a.gate ? gate_at<TB>(g[i].f[j], a.act).a : 1.f, y[i].f[j]);
                 }
                 store8(ry, (uint32_t)(t.slot * a.res_stride + col[i]) * (uint32_t)sizeof(TR) | (live && in[i] ? 0u : kOOB), y[i],
                        TR{});
@@ -423,9 +435,9 @@ __global__ __launch_bounds__(WT ? WT : 256, WT == 512 && !FULL && sizeof(TB) == 
                 for (int j = 0; j < 8; ++j) {
                     const float v = a.post == CBW_NORM_NONE ? u[i].f[j] : in[i] ? (u[i].f[j] - st.z) * st.w : 0.f;
                     const float z = fmaf(v, w.f[j], b.f[j]);
-                    const float act = a.gate ? gate_value(g[i].f[j], a.act) : 1.f;
-                    const float da = a.act == CBW_GATE_SIGMOID ? act * (1.f - act) : 1.f;
-                    dg.f[j] = gy[i].f[j] * s.f[j] * z * da;
+                    const Gate gate = a.gate ? gate_at<TB>(g[i].f[j], a.act) : Gate{1.f, 1.f};
+                    const float act = gate.a;
+                    dg.f[j] = gy[i].f[j] * s.f[j] * z * gate.da;
                     if (FULL) acc[NG_SCALE][i].f[j] = fmaf(gy[i].f[j] * act, z, acc[NG_SCALE][i].f[j]);
                     const float dz = gy[i].f[j] * s.f[j] * act;
                     acc[NG_W_POST][i].f[j] = fmaf(dz, v, acc[NG_W_POST][i].f[j]);

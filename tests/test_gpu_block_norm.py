@@ -278,3 +278,29 @@ def test_binding_refuses():
         a = {**ok, **bad}
         with pytest.raises(cb.CbwError):
             cb.block_norm_fwd(d, a["x"], a["u"], a["gate"], None, a["y"], a["h"], st)
+
+
+@pytest.mark.parametrize("rows,C", [(9, 64), (3, 4104), (2, 16384)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gates_far_out(rows, C, dtype):
+    """The sigmoid and its derivative keep their own relative accuracy however
+    far out the gate is.  With neither norm nor scale y - x = a u, dgate = dy u
+    a', du = dy a.  float32: an exponential (1 ulp), an addition, a division
+    and up to five products: 32 * 2^-24.  bf16: its own rounding, and 2^-14 for
+    a faster exponential, whose argument is rounded (at most 88 * 1.5 * 2^-24).
+    Past 87 the derivative leaves float32's normal range."""
+    g = torch.Generator().manual_seed(23)
+    gate = torch.cat([torch.linspace(-100, 100, rows * C // 2), 12 * torch.randn(rows * C // 2, generator=g)])
+    gate = gate[torch.randperm(rows * C, generator=g)].view(rows, C).to(DT[dtype])
+    u, dy = (torch.randn((rows, C), generator=g).to(DT[dtype]) for _ in range(2))
+    d = cb.NormDesc.make(rows, C, "none", "none", "sigmoid", 1, dtype, "f32", EPS)
+    G, U, DY, x = gate.cuda(), u.cuda(), dy.float().cuda(), torch.zeros((rows, C), device="cuda")
+    y, dx, du, dg = torch.empty_like(x), torch.empty_like(x), torch.empty_like(U), torch.empty_like(G)
+    st = torch.empty((rows, 4), device="cuda")
+    cb.block_norm_fwd(d, x, U, G, None, y, None, st)
+    cb.block_norm_bwd(d, y, U, G, None, st, DY, None, dx, du, dg, None, cb.norm_workspace(d))
+    near = 32 * ref.U32 if dtype == "f32" else 2.0 ** -14
+    a = torch.sigmoid(gate.double())
+    da = a * torch.sigmoid(-gate.double())
+    for name, got, want in (("y", y, a * u.double()), ("dgate", dg, dy.double() * u.double() * da), ("du", du, dy.double() * a)):
+        ref.check(got, want, near * want.abs(), name)
