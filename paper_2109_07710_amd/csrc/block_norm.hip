@@ -611,7 +611,7 @@ NormSplit norm_split(const cbw_norm_desc* d)
     s.grid = (int)std::max<int64_t>(1, std::min<int64_t>(steps, most));
     if (d->gate_act != CBW_GATE_NONE && d->gate_rows > 1) {
         s.group_rows = std::min(d->gate_rows, d->rows);
-        s.groups = std::max<int64_t>(1, (d->rows + d->gate_rows - 1) / d->gate_rows);
+        s.groups = d->rows > 0 ? (d->rows - 1) / d->gate_rows + 1 : 1;   // (gate_rows may be its type's largest value)
     } else {
         s.group_rows = d->rows;
         s.groups = 1;

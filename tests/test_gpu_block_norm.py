@@ -304,3 +304,20 @@ def test_gates_far_out(rows, C, dtype):
     da = a * torch.sigmoid(-gate.double())
     for name, got, want in (("y", y, a * u.double()), ("dgate", dg, dy.double() * u.double() * da), ("du", du, dy.double() * a)):
         ref.check(got, want, near * want.abs(), name)
+
+
+def test_gate_row_for_more_rows_than_there_can_be():
+    """gate_rows at the end of its type: one gate row serves all rows, as with gate_rows = rows."""
+    rows, C = 300, 72
+    t, p = _draw(rows, C, "rms", "rms", "sigmoid", rows, "bf16", "bf16", False, False, True, 24)
+    params = cb.NormParams(*(None if p[k] is None else p[k].cuda() for k in PARAMS))
+    x, u, g, dy, dh = (t[k].cuda() for k in ("x", "u", "gate", "dy", "dh"))
+    outs = []
+    for gate_rows in (rows, (1 << 63) - 1):
+        d = cb.NormDesc.make(rows, C, gate="sigmoid", gate_rows=gate_rows, eps=EPS)
+        y, h, st = torch.empty_like(x), torch.empty_like(u), torch.empty((rows, 4), device="cuda")
+        cb.block_norm_fwd(d, x, u, g, params, y, h, st)
+        dx, du, dg = torch.empty_like(x), torch.empty_like(u), torch.empty_like(g)
+        cb.block_norm_bwd(d, y, u, g, params, st, dy, dh, dx, du, dg, None, cb.norm_workspace(d))
+        outs.append((y, h, st, dx, du, dg))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
