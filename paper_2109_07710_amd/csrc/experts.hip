@@ -831,10 +831,10 @@ hipError_t launch_rows(const ExpertArgs& a, hipStream_t s)
     if constexpr (BF16) {
         if (mean >= 160 && likely_tiles(a, 256, P, 256) >= 200) return launch_tiles<T, KIND, 256, 256, 2, 4>(a, s);
         if (mean > 16 && likely_tiles(a, 128, P, 128) >= 200) return launch_tiles<T, KIND, 128, 128, 2, 2>(a, s);
+        if (mean > 64) return launch_stream<T, KIND, 64, 4, 4, 2>(a, s);   // (float32: the matrix unit would be the bound)
     } else {
         if (mean > 16 && likely_tiles(a, 64, P, 64) >= 400) return launch_tiles<T, KIND, 64, 64, 2, 2>(a, s);
     }
-    if (BF16 && mean > 64) return launch_stream<T, KIND, 64, 4, 4, 2>(a, s);   // (float32: the matrix unit would be the bound)
     if (likely_tiles(a, 16, P, 64) >= 192) return launch_stream<T, KIND, 64, 1, 4, 2>(a, s);
     return launch_stream<T, KIND, 32, 1, 8, 3>(a, s);
 }
