@@ -362,3 +362,53 @@ def test_more_workgroups_than_one_axis_takes(product):
     for e in (0, 63, 64, 500, 1023):
         we, xe = (w[e].t() if fwd else w[e]).cpu().double(), x[e:e + 1].cpu().double()
         ref.check(out[e:e + 1], xe @ we, (R + 4) * ref.U32 * (xe.abs() @ we.abs()), "expert %d" % e)
+
+
+def _part_rows(d):
+    """Bounds of the rows of a part, from the workspace: it holds 2 rows / part slots of K * C sums."""
+    slots = cb.cbw_expert_workspace_size(d) // (4 * d.C * d.K)
+    assert slots > 0
+    return 2 * d.rows // (slots + 1) + 1, 2 * d.rows // slots
+
+
+def _around(E, lengths):
+    """Offsets of E experts of which only `lengths` (expert: rows) have rows."""
+    off = [0]
+    for e in range(E):
+        off.append(off[-1] + lengths.get(e, 0))
+    return off
+
+
+# (rows, C, K, the experts' lengths, number of experts).  The part length
+# follows from the capacity `rows`, which the lengths need not fill.
+SPLIT = [
+    (9300, 72, 40, {0: 4000, 2: 1, 3: 3299, 4: 600, 5: 1400}, 6),
+    (9300, 72, 40, {0: 3299, 1: 400, 3: 517, 5: 1}, 6),
+    # split experts on both sides of the 64th, whole ones between them
+    (108000, 24, 16, {**{e: 3 * e + 1 for e in range(5, 70, 2)}, 2: 1500, 62: 700, 63: 514, 64: 5000, 66: 1025, 69: 600}, 70),
+    # tiles of 256 x 256 (bf16)
+    (16400, 520, 520, {**{e: 4 * e for e in range(4, 40)}, 0: 3000, 41: 1026, 50: 2049, 63: 1023}, 64),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,C,K,lengths,E", SPLIT, ids=lambda v: str(v) if isinstance(v, int) else "")
+def test_parts_of_several_experts(rows, C, K, lengths, E, dtype):
+    """At least two experts are taken in parts and at least one is not, twice
+    over a workspace that held other sums: within the bound, and the same bits."""
+    print("[case]", dtype, rows, C, K, E, flush=True)
+    off = _around(E, lengths)
+    assert off[-1] <= rows
+    d = cb.ExpertDesc.make(E, rows, C, K, dtype)
+    lo, hi = _part_rows(d)
+    assert sum(n > hi for n in lengths.values()) >= 2 and any(0 < n <= lo for n in lengths.values())
+    x, _, dy, _ = _draw(off, rows, C, K, dtype, 11)
+    o = torch.tensor(off, dtype=torch.int32, device="cuda")
+    got = []
+    for fill in (0, 255):
+        ws = torch.full((cb.cbw_expert_workspace_size(d),), fill, dtype=torch.uint8, device="cuda")
+        dW = torch.full((E, K, C), float("nan"), device="cuda")
+        cb.expert_bwd_weight(d, x.cuda(), dy.cuda(), o, dW, ws)
+        got.append(dW)
+    assert torch.equal(*got)
+    ref.check(got[0], *ref.expert_bwd_weight(x, dy, off), "dW")
