@@ -321,3 +321,66 @@ def test_gate_row_for_more_rows_than_there_can_be():
         cb.block_norm_bwd(d, y, u, g, params, st, dy, dh, dx, du, dg, None, cb.norm_workspace(d))
         outs.append((y, h, st, dx, du, dg))
     assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def _statistics_bound(v, err, kind, r):
+    """Bounds of what the kernel's mean and r of the rows v (64 bits, each
+    value known to within err) may be off by: the mean's from its terms; r's
+    relative one is half the mean square's, which changes by at most twice the
+    product of the deviations' and the errors' root mean squares."""
+    err = err + ref.ROW * v.abs().mean(1, keepdim=True)
+    mean = err.mean(1) if kind == "layer" else torch.zeros(v.shape[0], dtype=torch.float64)
+    return mean, r * (2 * r * err.square().mean(1).sqrt() + ref.ROW)
+
+
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("types", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")], ids="-".join)
+@pytest.mark.parametrize("kinds", [("rms", "rms"), ("layer", "layer"), ("layer", "none"), ("none", "layer"), ("rms", "layer")],
+                         ids="-".join)
+def test_statistics(size, types, kinds):
+    """All four columns: mean and r of y and of u, zeros where there is no norm."""
+    rows, C = size
+    pre, post = kinds
+    print("[case]", rows, C, *kinds, *types, flush=True)
+    t, p = _draw(rows, C, pre, post, "linear", 1, *types, True, True, True, 21, 0.5)
+    d = cb.NormDesc.make(rows, C, pre, post, "linear", 1, *types, EPS)
+    params = cb.NormParams(*(None if p[k] is None else p[k].cuda() for k in PARAMS))
+    x, u, g = (t[k].cuda() for k in ("x", "u", "gate"))
+    h = None if pre == "none" else torch.empty_like(u)
+    st = torch.full((rows, 4), float("nan"), device="cuda")
+    cb.block_norm_fwd(d, x, u, g, params, torch.empty_like(x), h, st)
+    got = st.cpu().double()
+    want = ref.norm_fwd(t["x"], t["u"], t["gate"], p, pre, post, "linear", 1, EPS)
+    y, y_err = want["y"]
+    for at, v, err, kind, mu, r in ((0, y, y_err, pre, want.get("mu"), want.get("r")),
+                                    (2, t["u"].double(), 0 * y, post, want["mu_u"], want["r_u"])):
+        if kind == "none":
+            assert (got[:, at:at + 2] == 0).all()
+            continue
+        mean_off, r_off = _statistics_bound(v, err, kind, r[:, 0])
+        assert ((got[:, at] - mu[:, 0]).abs() <= mean_off).all(), "mean"
+        assert ((got[:, at + 1] - r[:, 0]).abs() <= r_off).all(), "r"
+
+
+@pytest.mark.parametrize("C", [136, 520, 2056, 8200, 16384])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pre,post", [("rms", "rms"), ("layer", "layer"), ("rms", "layer")])
+def test_backward_from_the_forward_statistics(C, dtype, pre, post):
+    """A step as a program makes it: the backward pass reads the statistics
+    that the forward pass wrote.  The stream is float32, so that y is stored to
+    within the bounds' own size."""
+    rows = 5
+    t, p = _draw(rows, C, pre, post, "sigmoid", 1, dtype, "f32", True, True, True, 22, 0.25)
+    d = cb.NormDesc.make(rows, C, pre, post, "sigmoid", 1, dtype, "f32", EPS)
+    P = {k: v.cuda() for k, v in p.items()}
+    params = cb.NormParams(*(P[k] for k in PARAMS))
+    x, u, g, dy, dh = (t[k].cuda() for k in ("x", "u", "gate", "dy", "dh"))
+    y, h, st = torch.empty_like(x), torch.empty_like(u), torch.full((rows, 4), float("nan"), device="cuda")
+    cb.block_norm_fwd(d, x, u, g, params, y, h, st)
+    grads = {k: torch.full_like(v, float("nan")) for k, v in P.items()}
+    dx, du, dg = torch.empty_like(x), torch.empty_like(u), torch.empty_like(g)
+    cb.block_norm_bwd(d, y, u, g, params, st, dy, dh, dx, du, dg, cb.NormParams(*(grads[k] for k in PARAMS)),
+                      cb.norm_workspace(d))
+    want = ref.norm_bwd(y, t["u"], t["gate"], p, t["dy"], t["dh"], pre, post, "sigmoid", 1, EPS)
+    for name, got in (("dx", dx), ("du", du), ("dgate", dg), *grads.items()):
+        ref.check(got, *want[name], name)
