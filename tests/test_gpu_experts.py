@@ -412,3 +412,25 @@ def test_parts_of_several_experts(rows, C, K, lengths, E, dtype):
         got.append(dW)
     assert torch.equal(*got)
     ref.check(got[0], *ref.expert_bwd_weight(x, dy, off), "dW")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,C,K", [(40, 64, 64), (700, 128, 1056)])
+def test_relu_of_nonfinite_sums(rows, C, K, dtype):
+    """ReLU gives +0.0 for a NaN sum and for -infinity, and marks both dead;
+    +infinity stays and is live."""
+    off = [0, rows // 3, rows]
+    x, w, _, _ = _draw(off, rows, C, K, dtype, 12)
+    w[:, :, 0] = torch.where(torch.arange(K) % 2 == 0, 1.0, -1.0).to(w.dtype)
+    x[5, 0], x[rows - 1, 0], x[rows // 2, 1] = float("inf"), -float("inf"), float("nan")
+    d = cb.ExpertDesc.make(2, rows, C, K, dtype)
+    Y = torch.full((rows, K), -1.0, dtype=DT[dtype], device="cuda")
+    mask = torch.zeros((rows * K + 31) // 32, dtype=torch.int32, device="cuda")
+    cb.expert_fwd(d, x.cuda(), w.cuda(), torch.tensor(off, dtype=torch.int32, device="cuda"), Y, mask, cb.expert_workspace(d),
+                  cb.CBW_FLAG_RELU)
+    y = Y.cpu()
+    bits = y.view(torch.int16 if dtype == "bf16" else torch.int32)
+    assert torch.equal(y[5, 0::2], torch.full((K // 2,), float("inf"), dtype=y.dtype)) and (bits[5, 1::2] == 0).all()
+    assert torch.equal(y[-1, 1::2], torch.full((K // 2,), float("inf"), dtype=y.dtype)) and (bits[-1, 0::2] == 0).all()
+    assert (bits[rows // 2] == 0).all() and not y.isnan().any()
+    assert torch.equal(mask.cpu(), ref.bits(y > 0))
