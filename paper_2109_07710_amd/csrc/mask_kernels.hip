@@ -31,7 +31,7 @@ __global__ void mask_pack_kernel(const T* __restrict__ x, uint32_t* __restrict__
 {
     constexpr int E = Elem<T>::E;
     constexpr int L = 32 / E;
-    const int64_t v = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    const int64_t v = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x;
     uint32_t b = 0;
     if (v < nvec) {
         const int64_t e0 = v * E;
@@ -71,12 +71,13 @@ hipError_t launch_relu_mask_pack(int dtype, int64_t count, const void* x, uint32
     nvec = (nvec + L - 1) / L * L;  // whole words
     const int64_t blocks = (nvec + 255) / 256;
     if (blocks == 0) return hipSuccess;
+    // an axis of a launch takes 2^32 - 1 threads; more wrap without an error
+    const int64_t gx = blocks < 1 << 23 ? blocks : 1 << 23;
+    const dim3 grid((unsigned)gx, (unsigned)((blocks + gx - 1) / gx));
     if (dtype == 1)
-        mask_pack_kernel<uint16_t><<<(unsigned)blocks, 256, 0, stream>>>((const uint16_t*)x, bits, count, nvec,
-                                                                         relu != 0);
+        mask_pack_kernel<uint16_t><<<grid, 256, 0, stream>>>((const uint16_t*)x, bits, count, nvec, relu != 0);
     else
-        mask_pack_kernel<float><<<(unsigned)blocks, 256, 0, stream>>>((const float*)x, bits, count, nvec,
-                                                                      relu != 0);
+        mask_pack_kernel<float><<<grid, 256, 0, stream>>>((const float*)x, bits, count, nvec, relu != 0);
     return hipGetLastError();
 }
 
