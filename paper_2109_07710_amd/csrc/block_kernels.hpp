@@ -12,9 +12,10 @@ namespace cbw {
 
 // ------------------------------------------------------------ block norms
 
-// One row is held by a team of threads, vectors of 8 columns each: up to
-// kNormLanes lanes of a wave where the row fits two vectors a lane (several
-// rows to a workgroup then), else a whole workgroup of up to 16 waves.
+// One row is held by a team of threads, vectors of 8 columns each: up to 64
+// lanes of a wave where the row fits one vector a lane (several rows to a
+// workgroup then), else a whole workgroup of up to 16 waves, whose threads
+// take two vectors past 8192 columns.
 constexpr int kNormMaxC = 16384;
 
 struct NormShape {
@@ -73,7 +74,7 @@ struct NormBackArgs {
     const float* stats;
     void *dx, *du, *dgate;
     float* grads[NG_COUNT];     // where each gradient goes, null: not asked for
-    float* partial;             // [grid][asked for][C], null where one workgroup writes them itself
+    float* partial;             // [grid][NG_COUNT][C], those asked for first; null where one workgroup writes them itself
     float* gate_partial;        // [items][C] where a gate row's rows are split, else null
     int64_t rows, res_stride, block_stride, gate_stride, gate_rows;
     int C, pre, post, act;
@@ -118,8 +119,14 @@ hipError_t launch_expert_bwd_weight(int dtype, const ExpertArgs& a, bool large, 
 
 constexpr int kGradTable = 120;       // tensors per launch: the table travels in the kernel's arguments
 constexpr int kGradChunk = 16384;     // bytes a workgroup takes at a time
-constexpr int kGradMaxWgs = 1024;     // workgroups of a pass, shared out over its launches,
-constexpr int kGradMinWgs = 256;      // of which each has this many if it has the chunks
+// Workgroups of a pass, shared out over its launches, of which each has at
+// least kGradMinWgs if it has the chunks.  (us a clipping call with 512 | 1024 |
+// 2048 in all: 13 tensors, 59 MB: 38 | 37 | 37; 3 of 160 MB together: 104 |
+// 101 | 103; 48 of 2.1 GB: 1245 | 1280 | 1308; 400 of 80 MB: 66 | 66 | 63.  With
+// 128 | 256 | 512 at least: 300 packed tensors, 90 MB: 68.2 | 67.2 | 66.6; 400
+// of 80 MB: 67 | 66 | 64.)
+constexpr int kGradMaxWgs = 1024;
+constexpr int kGradMinWgs = 256;
 
 struct alignas(16) GradEntry {   // (copied by 16-byte vectors)
     const void* src;

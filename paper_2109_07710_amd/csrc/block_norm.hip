@@ -11,12 +11,15 @@
 //
 // Bound by memory: a row is read once into registers, where its statistics,
 // both norms and every gradient are computed, and written once (16384 rows of
-// 4096, bf16, RMS norms, a gate of its own for each value: forward 135 us, 4.95
-// TB/s, backward 244 us, 4.4 TB/s; 100352 rows of 256, layer norms, float32
-// stream, one gate row for 3136: backward 109 us, 4.25 TB/s).  One vector of 8
-// columns a thread: with two, half as many waves hid less of the loads'
-// latency (backward 374 us).  Statistics
-// are two-pass (the mean, then the squares about it) in float32; y and h are
+// 4096, bf16, RMS norms, a gate of its own for each value: forward 129 us, 5.2
+// TB/s, backward 237 us, 4.5 TB/s; with a float32 stream 173 and 313, float32
+// throughout 246 and 473; 100352 rows of 256, layer norms, float32 stream, one
+// gate row for 3136: backward 109 us, 4.25 TB/s).  One vector of 8 columns a
+// thread: with two, half as many waves hid less of the loads' latency
+// (backward 374 us).  Rows of more than 8192 columns have two, and their
+// backward pass spills registers (4096 rows of 16384, bf16: forward 148 us, 4.5
+// TB/s, backward 293, 3.7 TB/s, with biases and scale 816).  Statistics are
+// two-pass (the mean, then the squares about it) in float32; y and h are
 // rounded once each, h from the unrounded y.  The parameters' gradients are
 // summed over a workgroup's rows in registers and over the workgroups by a
 // second kernel, in a fixed order.
@@ -292,7 +295,11 @@ __global__ __launch_bounds__(WT ? WT : 256) void norm_fwd_kernel(NormArgs a, int
 }
 
 // FULL: gradients of biases or the scale are asked for as well (their sums
-// take registers that the usual call has no use for).
+// take registers that the usual call has no use for).  The bound on registers
+// keeps four waves to a SIMD where they nearly fit (us, 16384 rows of 4096,
+// with the bound | without: float32 stream 313 | 339, bf16 238 | 238; not kept
+// for FULL, 337 | 302, with a float32 stream 496 | 360, nor for a float32 block,
+// 462 | 473).
 template <typename TR, typename TB, int WT, int VPT, bool FULL>
 __global__ __launch_bounds__(WT ? WT : 256, WT == 512 && !FULL && sizeof(TB) == 2 ? 4 : 1) void norm_bwd_kernel(NormBackArgs a, int team)
 {

@@ -18,15 +18,20 @@
 //
 // Every workgroup finds its experts and tiles itself: a wave scans the group
 // lengths (E + 1 offsets, in the cache) and looks its own number up.  The
-// grid covers the most tiles any lengths can give; surplus workgroups leave.
+// tiled kernel has as many workgroups as are resident, which go through the
+// tiles in turn; the streaming kernel has one for every tile that any lengths
+// could give, and the surplus ones leave.
 //
 // Bound by the matrix cores where an expert has some hundred rows (16384 rows
 // over 8 experts, 2048 -> 8192 features, bf16: 502 us, 1095 TFLOP/s; with groups
 // of whole tiles 475 us, 1155), by reading the filters where it has few (12
-// rows over 32 experts, 2048 -> 1408: 14.6 us, 4.0 TB/s, filters read from memory;
-// 10.5 to 13 where calls in turn leave part of them in the 256 MB cache).  The weight gradient of narrow experts takes its products and
-// the writing of its results in turn (64 uneven experts, 32768 rows, 2048 ->
-// 1408: 310 to 334 us, 3.1 to 2.9 TB/s beside 610 to 565 TFLOP/s).
+// rows over 32 experts, 2048 -> 1408: 14.6 to 15.1 us, 4.0 TB/s, filters read from
+// memory; 10.5 to 13 where calls in turn leave part of them in the 256 MB
+// cache).  The weight gradient of narrow experts takes its products and the
+// writing of its results in turn (64 uneven experts, 32768 rows, 2048 -> 1408:
+// 310 to 343 us, 3.1 to 2.8 TB/s beside 610 to 550 TFLOP/s).  float32: 8192
+// rows over 8 experts, 1024 -> 2048, forward 292 us, data 303, weight 296,
+// 118 to 113 TFLOP/s.
 #include "common.hpp"
 #include "block_kernels.hpp"
 #include "tiles.hpp"
@@ -160,9 +165,8 @@ struct Operand {
 
     // Placement of the 16-byte chunks of an LDS row.  The LDS serves 256 bytes
     // (all banks) a cycle.  Along: a fragment read takes one chunk of 16
-    // consecutive rows per cycle; with rows of 128 bytes, of which two share
-    // the banks, the chunk is moved by the row's bits 1 to 3, with rows of 64
-    // bytes by its bits 2 and 3.  Across, bf16: a transposing read takes 32
+    // consecutive rows per cycle; of its rows of 128 bytes two share the
+    // banks, so the chunk is moved by the row's bits 1 to 3.  Across, bf16: a transposing read takes 32
     // bytes of rows b .. b+3 and b+8 .. b+11 per cycle: eight chunk pairs that
     // must not share banks (tiles of 64 columns: rows of 128 bytes, two of
     // them to the banks; of 32: four).  Across, float32: 64 bytes of rows 4 apart.
@@ -816,12 +820,20 @@ int64_t likely_tiles(const ExpertArgs& a, int tile, int P, int width)
 // stream, 64 rows): 16384 rows, 8 experts, 2048 -> 8192: 511 | 653 | - | -;
 // 6935 rows, 36 experts, 1736 -> 1312: 52 | 69 | 141 | 105; 3676, 3, 264 ->
 // 1576: 14 | 12 | 37 | 26; 256, 8, 2048 -> 8192: 52 | 45 | 52 | 54; 755, 1, 2664
-// -> 536: 57 | 38 | 14 | 13; 2108, 46, 848 -> 152: 22 | 14 | 7 | 7; 12, 32, 2048
+// -> 536: 57 | 38 | 14 | 13 (15.4 in a later run); 2108, 46, 848 -> 152: 22 | 14 | 7 | 7; 12, 32, 2048
 // -> 1408: 43 | 26 | 12 | 13.  Few tiles of 64 features: 16 rows, 1 expert, 8192
 // -> 512: 18, and 10 with 32 features and eight waves.  (The small ones' filters
 // lay in the caches.  From memory, 64 features and four waves | 32 and eight:
 // 12 rows, 32 experts, 2048 -> 1408: 15.7 | 16.9; 300, 64, 1024 -> 512: 15 | 22;
 // 1, 1, 2048 -> 8192: 10.3 | 9.5.)
+//
+// float32, forward, from memory (us, 64 x 64 tiles | stream, 16 rows; in
+// brackets the tiles of 64 x 64, of which the rule asks for 400): 640 rows, 16
+// experts, 2048 -> 256 (64): 50 | 18; 1000, 32, 512 -> 512 (256): 16.7 | 17.2;
+// 1024, 8, 1024 -> 1024 (256): 40 | 38; 300, 4, 4096 -> 4096 (512): 146 | 137;
+// 1800, 8, 1024 -> 1024 (512): 41 | 56; 4096, 1, 512 -> 512 (512): 23 | 36;
+// 2000, 64, 256 -> 1024 (1024): 25 | 31.  One wide group of few tiles goes the
+// slower way: 2000, 1, 512 -> 512 (256): 14.8 | 18.3.
 template <typename T, int KIND>
 hipError_t launch_rows(const ExpertArgs& a, hipStream_t s)
 {
@@ -858,7 +870,10 @@ hipError_t launch_rows(const ExpertArgs& a, hipStream_t s)
 // and would alone take half the call's time (64 uneven experts, 32768 rows,
 // 2048 -> 1408, the longest 5591: 377 us whole, 332 in the parts of half a
 // workgroup's share that follow; 8 even ones of 2048 rows, 1024 -> 1024: 44
-// whole, 73 by 1024).
+// whole, 73 by 1024).  (The small ones' rows lay in the caches: the 17 and 26
+// us calls take 20 and 30 from memory.)  The launch that adds parts up is
+// made wherever the capacity exceeds a part's rows, also where no expert turns
+// out to have as many.
 ExpertPlan expert_plan(const cbw_expert_desc* d)
 {
     ExpertPlan p{};
