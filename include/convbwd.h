@@ -43,8 +43,9 @@
  * Beside the convolution's operations stand those of a block with several
  * experts (a layer in which every group of rows has a filter of its own), at
  * the end of this header: the products grouped by expert with their two
- * gradients, the norms around a block with its gate and residual scale, and
- * the norm and clipping of all gradients.  They keep the same conventions.
+ * gradients, the gated layer's products and their gradients, the norms around
+ * a block with its gate and residual scale, and the norm and clipping of all
+ * gradients.  They keep the same conventions.
  */
 #ifndef CONVBWD_H
 #define CONVBWD_H
@@ -404,6 +405,56 @@ int expert_bwd_data(const cbw_expert_desc* desc, const void* dY, const void* W, 
  * rows' partial sums are added in a fixed order. */
 int expert_bwd_weight(const cbw_expert_desc* desc, const void* X, const void* dY, const int32_t* offsets, float* dW,
                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------ gated products grouped by expert
+ *
+ * A layer with two filters for every expert, gate and up: W is [E][2][K][C],
+ * the gate's first.  Its rows are grouped as those of the products above.
+ *
+ *   g[r,k] = sum_c X[r,c] W[e,0,k,c],  u[r,k] = sum_c X[r,c] W[e,1,k,c]
+ *   H[r,k] = act(g[r,k]) u[r,k]
+ *
+ * Backward, from the gradient dY of the next filter's output, W2 [E][C][K]:
+ *
+ *   dH[r,k] = sum_c dY[r,c] W2[e,c,k]
+ *   dg = dH u act'(g),  du = dH act(g)
+ *
+ * One expert with all rows is an ordinary gated layer.  W is also a layer of
+ * 2K features ([E][2K][C]) and GU, the rows (g, u), its output: the remaining
+ * gradients are expert_bwd_weight and expert_bwd_data with K twice as large
+ * on dGU, and expert_bwd_weight of the next layer on H and dY.
+ *
+ * act: relu (NaN gives 0, as CBW_FLAG_RELU), sigmoid, silu = g sigmoid(g),
+ * gelu in the form g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))). */
+enum { CBW_ACT_RELU = 0, CBW_ACT_SIGMOID = 1, CBW_ACT_SILU = 2, CBW_ACT_GELU = 3 };
+typedef struct {
+    int32_t E;               /* experts, at most CBW_MAX_EXPERTS               */
+    int32_t C;               /* features that the product runs over: X's, dY's */
+    int32_t K;               /* features of the gated layer                    */
+    int32_t dtype;           /* cbw_dtype of all tensors                       */
+    int32_t act;             /* CBW_ACT_*                                      */
+    int32_t reserved;        /* 0                                              */
+    int64_t rows;            /* rows of X, dY, H, GU (a capacity); 0 is allowed */
+    int64_t x_stride;        /* elements between rows: X, dY                   */
+    int64_t h_stride;        /* H                                              */
+    int64_t gu_stride;       /* GU and dGU, at least 2K                        */
+} cbw_gated_desc;
+
+/* Host-only check.  CBW_ERR_UNSUPPORTED as cbw_validate_expert_desc for a
+ * layer of 2K features. */
+int cbw_validate_gated_desc(const cbw_gated_desc* desc);
+
+/* H[rows][K] and, unless GU is NULL, GU[rows][2K] from X[rows][C] and
+ * W[E][2][K][C].  float32 accumulation; H is rounded once, from the unrounded
+ * g and u.  Rows of no expert are neither read nor written. */
+int expert_gated_fwd(const cbw_gated_desc* desc, const void* X, const void* W, const int32_t* offsets, void* H,
+                     void* GU, void* stream);
+
+/* dGU[rows][2K] = (dg, du) and, unless H is NULL, H once more (from GU's
+ * rounded values, for a program that did not keep it) from dY[rows][C],
+ * W2[E][C][K] and the GU of the forward pass.  dH is not rounded.  dGU may be GU. */
+int expert_gated_bwd(const cbw_gated_desc* desc, const void* dY, const void* W2, const int32_t* offsets, const void* GU,
+                     void* dGU, void* H, void* stream);
 
 /* ------------------------------- norms around a block, gate, residual scale
  *

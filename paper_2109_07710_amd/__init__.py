@@ -28,6 +28,7 @@ CBW_FLAG_NO_SKIP = 1
 CBW_FLAG_SKIP_X_BLOCKS = 2
 CBW_FLAG_RELU = 4
 CBW_MAX_EXPERTS = 1024
+CBW_ACT_RELU, CBW_ACT_SIGMOID, CBW_ACT_SILU, CBW_ACT_GELU = 0, 1, 2, 3
 CBW_NORM_NONE, CBW_NORM_RMS, CBW_NORM_LAYER = 0, 1, 2
 CBW_GATE_NONE, CBW_GATE_LINEAR, CBW_GATE_SIGMOID = 0, 1, 2
 CBW_GRAD_NORM_2, CBW_GRAD_NORM_INF = 0, 1
@@ -39,6 +40,7 @@ EXPORTS = ("cbw_status_string", "cbw_validate_desc", "cbw_mask_words", "cbw_dy_m
            "cbw_read_live_lists",
            "cbw_read_occupancy", "cbw_set_profile_events",
            "cbw_validate_expert_desc", "cbw_expert_workspace_size", "expert_fwd", "expert_bwd_data", "expert_bwd_weight",
+           "cbw_validate_gated_desc", "expert_gated_fwd", "expert_gated_bwd",
            "cbw_validate_norm_desc", "cbw_norm_workspace_size", "block_norm_fwd", "block_norm_bwd",
            "cbw_grad_workspace_size", "grad_norm", "grad_clip")
 
@@ -78,6 +80,17 @@ class ExpertDesc(ctypes.Structure):
     def make(cls, E, rows, C, K, dtype="bf16", x_stride=None, y_stride=None):
         return cls(E, C, K, _DTYPES[dtype], rows, C if x_stride is None else x_stride,
                    K if y_stride is None else y_stride)
+
+
+class GatedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("E", "C", "K", "dtype", "act", "reserved")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "x_stride", "h_stride", "gu_stride")]
+
+    @classmethod
+    def make(cls, E, rows, C, K, act="silu", dtype="bf16", x_stride=None, h_stride=None, gu_stride=None):
+        acts = {"relu": CBW_ACT_RELU, "sigmoid": CBW_ACT_SIGMOID, "silu": CBW_ACT_SILU, "gelu": CBW_ACT_GELU}
+        return cls(E, C, K, _DTYPES[dtype], acts[act], 0, rows, C if x_stride is None else x_stride,
+                   K if h_stride is None else h_stride, 2 * K if gu_stride is None else gu_stride)
 
 
 class NormDesc(ctypes.Structure):
@@ -180,13 +193,16 @@ def lib():
     L.cbw_read_live_lists.argtypes = [dp, vp, sz, ctypes.c_int, vp, i32p, i32p, vp]
     L.cbw_read_occupancy.argtypes = [dp, vp, sz, vp, i32p, i32p, i32p, i32p, vp]
     L.cbw_set_profile_events.argtypes = [ctypes.c_int, vp, vp]
-    ep, np_, pp, gp = (ctypes.POINTER(t) for t in (ExpertDesc, NormDesc, NormParams, _Grad))
+    ep, hp, np_, pp, gp = (ctypes.POINTER(t) for t in (ExpertDesc, GatedDesc, NormDesc, NormParams, _Grad))
     u32, i32 = ctypes.c_uint32, ctypes.c_int32
     L.cbw_validate_expert_desc.argtypes = [ep]
     L.cbw_expert_workspace_size.argtypes = [ep, ctypes.POINTER(sz)]
     L.expert_fwd.argtypes = [ep, vp, vp, vp, vp, vp, vp, sz, u32, vp]
     L.expert_bwd_data.argtypes = [ep, vp, vp, vp, vp, vp, vp, sz, vp]
     L.expert_bwd_weight.argtypes = [ep, vp, vp, vp, vp, vp, sz, vp]
+    L.cbw_validate_gated_desc.argtypes = [hp]
+    L.expert_gated_fwd.argtypes = [hp, vp, vp, vp, vp, vp, vp]
+    L.expert_gated_bwd.argtypes = [hp, vp, vp, vp, vp, vp, vp, vp]
     L.cbw_validate_norm_desc.argtypes = [np_]
     L.cbw_norm_workspace_size.argtypes = [np_, ctypes.POINTER(sz)]
     L.block_norm_fwd.argtypes = [np_, vp, vp, vp, pp, vp, vp, vp, vp]
@@ -283,6 +299,16 @@ def _whole(t, numel, dtype):
     if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous():
         raise ValueError("expected a contiguous %s tensor of %d elements" % (dtype, numel))
     return t.data_ptr()
+
+
+def _here(*tensors):
+    """Refuses tensors of another device than the current one, on which the
+    kernels would run."""
+    import torch
+    device = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else None
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != device:
+            raise ValueError("expected tensors of the current device, %d, got one of %s" % (device, t.device))
 
 
 def _stream(stream):
@@ -496,9 +522,10 @@ def expert_workspace(desc, device="cuda"):
     return _workspace_of(cbw_expert_workspace_size(desc), device)
 
 
-def _filters(d, W, dtype):
-    if W.shape != (d.E, d.K, d.C):
-        raise ValueError("expected filters of shape (%d, %d, %d), got %s" % (d.E, d.K, d.C, tuple(W.shape)))
+def _filters(d, W, dtype, shape=None):
+    shape = (d.E, d.K, d.C) if shape is None else shape
+    if W.shape != shape:
+        raise ValueError("expected filters of shape %s, got %s" % (shape, tuple(W.shape)))
     return _whole(W, 0, dtype)
 
 
@@ -531,6 +558,35 @@ def expert_bwd_weight(desc, X, dY, offsets, dW, ws, stream=None):
     _check(lib().expert_bwd_weight(ctypes.byref(d), _rows(X, rows, C, d.x_stride, dt), _rows(dY, rows, K, d.y_stride, dt),
                                    _whole(offsets, d.E + 1, types[2]), _filters(d, dW, types[CBW_F32]), _ptr(ws),
                                    _nbytes(ws), _stream(stream)), "expert_bwd_weight")
+
+
+# ------------------------------------------ gated products grouped by expert
+
+def cbw_validate_gated_desc(desc):
+    return lib().cbw_validate_gated_desc(ctypes.byref(desc))
+
+
+def expert_gated_fwd(desc, X, W, offsets, H, GU=None, stream=None):
+    """H = act(g) u with (g, u) = X W[e]^T for the rows of every expert e, W
+    [E][2][K][C]; GU ([rows][2K], or None): g and u, for the backward pass."""
+    _here(X, W, offsets, H, GU)
+    d, types = desc, _types()
+    dt, rows, C, K = types[d.dtype], d.rows, d.C, d.K
+    _check(lib().expert_gated_fwd(ctypes.byref(d), _rows(X, rows, C, d.x_stride, dt), _filters(d, W, dt, (d.E, 2, K, C)),
+                                  _whole(offsets, d.E + 1, types[2]), _rows(H, rows, K, d.h_stride, dt),
+                                  _rows(GU, rows, 2 * K, d.gu_stride, dt), _stream(stream)), "expert_gated_fwd")
+
+
+def expert_gated_bwd(desc, dY, W2, offsets, GU, dGU, H=None, stream=None):
+    """dGU = (dH u act'(g), dH act(g)) with dH = dY W2[e], W2 [E][C][K]; dGU may
+    be GU.  H (or None): act(g) u once more."""
+    _here(dY, W2, offsets, GU, dGU, H)
+    d, types = desc, _types()
+    dt, rows, C, K = types[d.dtype], d.rows, d.C, d.K
+    _check(lib().expert_gated_bwd(ctypes.byref(d), _rows(dY, rows, C, d.x_stride, dt), _filters(d, W2, dt, (d.E, C, K)),
+                                  _whole(offsets, d.E + 1, types[2]), _rows(GU, rows, 2 * K, d.gu_stride, dt),
+                                  _rows(dGU, rows, 2 * K, d.gu_stride, dt), _rows(H, rows, K, d.h_stride, dt),
+                                  _stream(stream)), "expert_gated_bwd")
 
 
 # -------------------------------- norms around a block, gate, residual scale

@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "../../include/convbwd.h"
 #include "block_kernels.hpp"
@@ -63,6 +64,41 @@ ExpertArgs expert_args(const cbw_expert_desc* d, const void* p, const void* q, c
     a.E = d->E;
     a.C = d->C;
     a.K = d->K;
+    return a;
+}
+
+// ----------------------------------------------------------- gated products
+
+int gated_check(const cbw_gated_desc* d, const void* rows, const void* filters, const int32_t* offsets,
+                std::initializer_list<const void*> needed, const void* optional)
+{
+    const int st = cbw_validate_gated_desc(d);
+    if (st != CBW_OK) return st;
+    if (!offsets) return CBW_ERR_INVALID_ARG;
+    if (!aligned(offsets, 4) || !aligned(rows, 16) || !aligned(filters, 16) || !aligned(optional, 16)) return CBW_ERR_UNSUPPORTED;
+    // (tensors without rows may have no address)
+    if (d->rows > 0 && (!rows || !filters)) return CBW_ERR_INVALID_ARG;
+    for (const void* p : needed) {
+        if (d->rows > 0 && !p) return CBW_ERR_INVALID_ARG;
+        if (!aligned(p, 16)) return CBW_ERR_UNSUPPORTED;
+    }
+    return CBW_OK;
+}
+
+GatedArgs gated_args(const cbw_gated_desc* d, const void* filters, const void* rows, const int32_t* offsets)
+{
+    GatedArgs a{};
+    a.p = filters;
+    a.q = rows;
+    a.offsets = offsets;
+    a.rows = d->rows;
+    a.x_stride = d->x_stride;
+    a.h_stride = d->h_stride;
+    a.gu_stride = d->gu_stride;
+    a.E = d->E;
+    a.C = d->C;
+    a.K = d->K;
+    a.act = d->act;
     return a;
 }
 
@@ -246,6 +282,44 @@ int expert_bwd_weight(const cbw_expert_desc* desc, const void* X, const void* dY
     a.split_rows = plan.split_rows;
     a.slots = plan.slots;
     return hip_status(launch_expert_bwd_weight(desc->dtype, a, plan.large, static_cast<hipStream_t>(stream)));
+}
+
+int cbw_validate_gated_desc(const cbw_gated_desc* d)
+{
+    if (!d) return CBW_ERR_INVALID_ARG;
+    if (d->act < CBW_ACT_RELU || d->act > CBW_ACT_GELU || d->reserved != 0) return CBW_ERR_INVALID_ARG;
+    if (d->K <= 0 || d->h_stride < d->K || d->gu_stride / 2 < d->K) return CBW_ERR_INVALID_ARG;
+    if (d->K > 0x3fffffff) return CBW_ERR_UNSUPPORTED;
+    // the two filters are one of 2K features; H's rows are those of one of K
+    cbw_expert_desc both = {d->E, d->C, 2 * d->K, d->dtype, d->rows, d->x_stride, d->gu_stride};
+    cbw_expert_desc next = {d->E, d->C, d->K, d->dtype, d->rows, d->x_stride, d->h_stride};
+    const int st = cbw_validate_expert_desc(&both);
+    return st != CBW_OK ? st : cbw_validate_expert_desc(&next);
+}
+
+int expert_gated_fwd(const cbw_gated_desc* desc, const void* X, const void* W, const int32_t* offsets, void* H,
+                     void* GU, void* stream)
+{
+    const int st = gated_check(desc, X, W, offsets, {H}, GU);
+    if (st != CBW_OK) return st;
+    if (desc->rows == 0) return CBW_OK;
+    GatedArgs a = gated_args(desc, W, X, offsets);
+    a.h = H;
+    a.gu_out = GU;
+    return hip_status(launch_gated_fwd(desc->dtype, a, static_cast<hipStream_t>(stream)));
+}
+
+int expert_gated_bwd(const cbw_gated_desc* desc, const void* dY, const void* W2, const int32_t* offsets, const void* GU,
+                     void* dGU, void* H, void* stream)
+{
+    const int st = gated_check(desc, dY, W2, offsets, {GU, dGU}, H);
+    if (st != CBW_OK) return st;
+    if (desc->rows == 0) return CBW_OK;
+    GatedArgs a = gated_args(desc, W2, dY, offsets);
+    a.h = H;
+    a.gu_in = GU;
+    a.gu_out = dGU;
+    return hip_status(launch_gated_bwd(desc->dtype, a, static_cast<hipStream_t>(stream)));
 }
 
 int cbw_validate_norm_desc(const cbw_norm_desc* d)

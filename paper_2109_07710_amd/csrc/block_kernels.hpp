@@ -115,6 +115,21 @@ hipError_t launch_expert_fwd(int dtype, const ExpertArgs& a, hipStream_t s);
 hipError_t launch_expert_bwd_data(int dtype, const ExpertArgs& a, hipStream_t s);
 hipError_t launch_expert_bwd_weight(int dtype, const ExpertArgs& a, bool large, hipStream_t s);
 
+// ---------------------------------------------------------- gated products
+
+struct GatedArgs {
+    const void *p, *q;          // filters; the rows that the product reads
+    const int32_t* offsets;
+    void* h;                    // forward: always there
+    const void* gu_in;          // backward: the two sums
+    void* gu_out;               // the two sums (forward, null: not kept), their gradients
+    int64_t rows, x_stride, h_stride, gu_stride;
+    int E, C, K, act;
+};
+
+hipError_t launch_gated_fwd(int dtype, const GatedArgs& a, hipStream_t s);
+hipError_t launch_gated_bwd(int dtype, const GatedArgs& a, hipStream_t s);
+
 // ------------------------------------------------------- gradient clipping
 
 constexpr int kGradTable = 120;       // tensors per launch: the table travels in the kernel's arguments
