@@ -44,8 +44,8 @@
  * experts (a layer in which every group of rows has a filter of its own), at
  * the end of this header: the products grouped by expert with their two
  * gradients, the gated layer's products and their gradients, the norms around
- * a block with its gate and residual scale, and the norm and clipping of all
- * gradients.  They keep the same conventions.
+ * a block with its gate and residual scale, the norm and clipping of all
+ * gradients, and their orthogonalised update.  They keep the same conventions.
  */
 #ifndef CONVBWD_H
 #define CONVBWD_H
@@ -551,6 +551,44 @@ int grad_norm(const cbw_grad* grads, int32_t n, int32_t kind, float* norm, void*
  * (out == grad) is not touched when c is 1.  max_norm is not negative. */
 int grad_clip(const cbw_grad* grads, int32_t n, int32_t kind, float max_norm, float* norm, void* workspace,
               size_t workspace_bytes, void* stream);
+
+/* -------------------------------------------------- orthogonalised update
+ *
+ * For each matrix M of a batch (the gradients of the experts' filters [E][K][C],
+ * or a convolution's as K rows of R S C values), O = M's singular vectors with
+ * singular values near one, by Newton-Schulz steps:
+ *
+ *   X = M / (|M| + eps)                          (the 2-norm of all its values)
+ *   X = a X + (b A + c A A) X,  A = X X^T        (`steps` times)
+ *
+ * (or, the same, with A = X^T X from the right where it has more rows than
+ * columns).  A matrix of zeros gives zeros, one with a NaN or an infinity NaN
+ * throughout.  X is held in float32; with a float32 result the products take
+ * 22 bits of each value, with bf16 those before the last two steps 11. */
+typedef struct {
+    int32_t rows, cols, batch;          /* batch 0 is allowed                    */
+    int32_t dtype;                      /* cbw_dtype of M                        */
+    int32_t out_dtype;                  /* of O                                  */
+    int32_t steps;                      /* at least 1                            */
+    int64_t in_stride, out_stride;      /* elements between rows; a matrix begins
+                                           rows * stride after the one before    */
+    float a, b, c;                      /* for example 3.4445, -4.7750, 2.0315   */
+    float eps;                          /* finite, not negative                  */
+} cbw_ortho_desc;
+
+/* Host-only check.  CBW_ERR_UNSUPPORTED: more than 2^20 rows or columns, more
+ * than 16384 of both, over 100 steps, a stride over 2^31 elements, 2^22 tiles of
+ * 64 x 64 or more in all, coefficients that let a singular value grow past 4 or
+ * b A + c A A past 32 on the way. */
+int cbw_validate_ortho_desc(const cbw_ortho_desc* desc);
+
+/* Workspace bytes (host only): some 12 for each value of M, 8 for each of A. */
+int cbw_ortho_workspace_size(const cbw_ortho_desc* desc, size_t* bytes);
+
+/* M and O need the alignment of their type alone.  O may be M where types and
+ * strides are the same. */
+int grad_orthogonalize(const cbw_ortho_desc* desc, const void* M, void* O, void* workspace, size_t workspace_bytes,
+                       void* stream);
 
 #ifdef __cplusplus
 }

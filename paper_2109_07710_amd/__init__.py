@@ -42,7 +42,8 @@ EXPORTS = ("cbw_status_string", "cbw_validate_desc", "cbw_mask_words", "cbw_dy_m
            "cbw_validate_expert_desc", "cbw_expert_workspace_size", "expert_fwd", "expert_bwd_data", "expert_bwd_weight",
            "cbw_validate_gated_desc", "expert_gated_fwd", "expert_gated_bwd",
            "cbw_validate_norm_desc", "cbw_norm_workspace_size", "block_norm_fwd", "block_norm_bwd",
-           "cbw_grad_workspace_size", "grad_norm", "grad_clip")
+           "cbw_grad_workspace_size", "grad_norm", "grad_clip",
+           "cbw_validate_ortho_desc", "cbw_ortho_workspace_size", "grad_orthogonalize")
 
 _DTYPES = {"bf16": CBW_BF16, "f32": CBW_F32}
 
@@ -119,6 +120,17 @@ class NormParams(ctypes.Structure):
             raise ValueError("parameters of different sizes: %s" % sorted(sizes))
         self.size = sizes.pop() if sizes else None
         super().__init__(*(None if t is None else _typed(t, CBW_F32).data_ptr() for t in self.tensors))
+
+
+class OrthoDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "cols", "batch", "dtype", "out_dtype", "steps")] + \
+               [(n, ctypes.c_int64) for n in ("in_stride", "out_stride")] + [(n, ctypes.c_float) for n in ("a", "b", "c", "eps")]
+
+    @classmethod
+    def make(cls, rows, cols, batch=1, dtype="f32", out_dtype="f32", steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7,
+             in_stride=None, out_stride=None):
+        return cls(rows, cols, batch, _DTYPES[dtype], _DTYPES[out_dtype], steps, cols if in_stride is None else in_stride,
+                   cols if out_stride is None else out_stride, *coefficients, eps)
 
 
 class _Grad(ctypes.Structure):
@@ -210,6 +222,10 @@ def lib():
     L.cbw_grad_workspace_size.argtypes = [gp, i32, ctypes.POINTER(sz)]
     L.grad_norm.argtypes = [gp, i32, i32, vp, vp, sz, vp]
     L.grad_clip.argtypes = [gp, i32, i32, ctypes.c_float, vp, vp, sz, vp]
+    op = ctypes.POINTER(OrthoDesc)
+    L.cbw_validate_ortho_desc.argtypes = [op]
+    L.cbw_ortho_workspace_size.argtypes = [op, ctypes.POINTER(sz)]
+    L.grad_orthogonalize.argtypes = [op, vp, vp, vp, sz, vp]
     for name in EXPORTS:
         if name != "cbw_status_string" and name not in ("cbw_mask_words", "cbw_dy_mask_words"):
             getattr(L, name).restype = ctypes.c_int
@@ -661,3 +677,50 @@ def grad_clip(grads, max_norm, norm, ws, kind="2", stream=None):
     1e-6)); norm (float32, on the device) = the norm and that factor."""
     _check(lib().grad_clip(grads.array, len(grads.grads), _KINDS[kind], max_norm, _whole(norm, 2, _types()[CBW_F32]),
                            _ptr(ws), _nbytes(ws), _stream(stream)), "grad_clip")
+
+
+# ------------------------------------------------------ orthogonalised update
+
+def cbw_validate_ortho_desc(desc):
+    return lib().cbw_validate_ortho_desc(ctypes.byref(desc))
+
+
+def cbw_ortho_workspace_size(desc):
+    return _bytes("cbw_ortho_workspace_size", ctypes.byref(desc))
+
+
+def ortho_workspace(desc, device="cuda"):
+    """A uint8 device tensor of the size grad_orthogonalize needs."""
+    return _workspace_of(cbw_ortho_workspace_size(desc), device)
+
+
+def _matrices(t, d, stride, dtype):
+    """Device pointer of the matrices [batch][rows][cols], rows `stride`
+    elements apart throughout; one matrix may be without the first axis, and
+    further axes may be taken together as its columns ([K][R][S][C])."""
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    if t.dtype is not dtype:
+        raise ValueError("expected a %s tensor, got %s" % (dtype, t.dtype))
+    whole = d.batch * d.rows * d.cols
+    if stride == d.cols:
+        if t.numel() != whole or not t.is_contiguous():
+            raise ValueError("expected a contiguous tensor of %d matrices of %d x %d, got shape %s, strides %s" % (
+                d.batch, d.rows, d.cols, tuple(t.shape), t.stride()))
+    elif whole:
+        if tuple(t.shape) not in ((d.batch, d.rows, d.cols), (d.rows, d.cols) if d.batch == 1 else None):
+            raise ValueError("expected %d matrices of %d x %d, got shape %s" % (d.batch, d.rows, d.cols, tuple(t.shape)))
+        want = (d.rows * stride, stride, 1)[-t.dim():]
+        if any(n > 1 and s != w for n, s, w in zip(t.shape, t.stride(), want)):
+            raise ValueError("expected rows %d elements apart, got strides %s" % (stride, t.stride()))
+    return t.data_ptr()
+
+
+def grad_orthogonalize(desc, M, O, ws, stream=None):
+    """O = the matrices M with singular values near one, by the descriptor's
+    Newton-Schulz steps; O may be M."""
+    _here(M, O, ws)
+    d, types = desc, _types()
+    _check(lib().grad_orthogonalize(ctypes.byref(d), _matrices(M, d, d.in_stride, types[d.dtype]),
+                                    _matrices(O, d, d.out_stride, types[d.out_dtype]), _ptr(ws), _nbytes(ws), _stream(stream)),
+           "grad_orthogonalize")

@@ -216,6 +216,39 @@ int check_norm_call(const cbw_grad* grads, int32_t n, int32_t kind, bool with_ou
     return check_ws(ws, ws_bytes, work->ws_bytes());
 }
 
+// ------------------------------------------------------ orthogonalised update
+
+// Whether singular values from [0, 1] on keep within what the products' fp16
+// planes hold: p(v) = a v + b v^3 + c v^5 step by step, and b l + c l^2 over l = v^2.
+// The largest value of either over [0, top] is at an end or where the slope is zero.
+bool coefficients_stay(const cbw_ortho_desc* d)
+{
+    const double a = d->a, b = d->b, c = d->c;
+    double top = 1.0;
+    for (int k = 0; k < d->steps; ++k) {
+        auto p = [&](double v) { return std::fabs(v * (a + v * v * (b + v * v * c))); };
+        auto q = [&](double l) { return std::fabs(l * (b + l * c)); };
+        double next = p(top), poly = q(top * top);
+        // 5 c l^2 + 3 b l + a = 0
+        double roots[3] = {-1.0, -1.0, c != 0.0 ? -b / (2.0 * c) : -1.0};
+        if (c != 0.0) {
+            const double disc = 9.0 * b * b - 20.0 * a * c;
+            if (disc >= 0.0) {
+                roots[0] = (-3.0 * b + std::sqrt(disc)) / (10.0 * c);
+                roots[1] = (-3.0 * b - std::sqrt(disc)) / (10.0 * c);
+            }
+        } else if (b != 0.0) {
+            roots[0] = -a / (3.0 * b);
+        }
+        for (int i = 0; i < 2; ++i)
+            if (roots[i] > 0.0 && roots[i] < top * top) next = std::max(next, p(std::sqrt(roots[i])));
+        if (roots[2] > 0.0 && roots[2] < top * top) poly = std::max(poly, q(roots[2]));
+        if (!(next <= 4.0) || !(poly <= 32.0)) return false;
+        top = std::max(next, 1e-30);
+    }
+    return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -485,6 +518,72 @@ int grad_clip(const cbw_grad* grads, int32_t n, int32_t kind, float max_norm, fl
     // (without tensors one workgroup writes the norm, 0, and c)
     const int grid = work.chunks ? grad_grid(work.chunks, work.chunks) : 1;
     return hip_status(launch_grad_scale(table, (int)work.tensors, (int)work.chunks, kind, grid, partial, count, max_norm, norm, s));
+}
+
+int cbw_validate_ortho_desc(const cbw_ortho_desc* d)
+{
+    if (!d) return CBW_ERR_INVALID_ARG;
+    if (d->rows <= 0 || d->cols <= 0 || d->batch < 0 || !known_dtype(d->dtype) || !known_dtype(d->out_dtype) || d->steps < 1)
+        return CBW_ERR_INVALID_ARG;
+    if (d->in_stride < d->cols || d->out_stride < d->cols) return CBW_ERR_INVALID_ARG;
+    if (!std::isfinite(d->a) || !std::isfinite(d->b) || !std::isfinite(d->c)) return CBW_ERR_INVALID_ARG;
+    if (!(d->eps >= 0.f) || std::isinf(d->eps)) return CBW_ERR_INVALID_ARG;
+    if (std::max(d->rows, d->cols) > 1 << 20 || std::min(d->rows, d->cols) > 16384 || d->steps > 100) return CBW_ERR_UNSUPPORTED;
+    if (d->in_stride > (int64_t)1 << 31 || d->out_stride > (int64_t)1 << 31) return CBW_ERR_UNSUPPORTED;
+    if (((int64_t)d->rows + 127) / 64 * (((int64_t)d->cols + 127) / 64) * d->batch >= 1 << 22) return CBW_ERR_UNSUPPORTED;
+    return coefficients_stay(d) ? CBW_OK : CBW_ERR_UNSUPPORTED;
+}
+
+int cbw_ortho_workspace_size(const cbw_ortho_desc* desc, size_t* bytes)
+{
+    if (!bytes) return CBW_ERR_INVALID_ARG;
+    const int st = cbw_validate_ortho_desc(desc);
+    if (st != CBW_OK) return st;
+    *bytes = desc->batch ? ortho_plan(desc).ws_bytes : 0;
+    return CBW_OK;
+}
+
+int grad_orthogonalize(const cbw_ortho_desc* desc, const void* M, void* O, void* workspace, size_t workspace_bytes,
+                       void* stream)
+{
+    int st = cbw_validate_ortho_desc(desc);
+    if (st != CBW_OK) return st;
+    if (desc->batch == 0) return CBW_OK;   // (no matrices may have no address)
+    if (!M || !O) return CBW_ERR_INVALID_ARG;
+    if (M == O && (desc->dtype != desc->out_dtype || desc->in_stride != desc->out_stride)) return CBW_ERR_INVALID_ARG;
+    if (!aligned(M, desc->dtype == CBW_F32 ? 4 : 2) || !aligned(O, desc->out_dtype == CBW_F32 ? 4 : 2)) return CBW_ERR_UNSUPPORTED;
+    const OrthoPlan p = ortho_plan(desc);
+    if ((st = check_ws(workspace, workspace_bytes, p.ws_bytes)) != CBW_OK) return st;
+    char* ws = static_cast<char*>(workspace);
+    OrthoArgs a{};
+    a.m = M;
+    a.o = O;
+    a.in_stride = desc->in_stride;
+    a.out_stride = desc->out_stride;
+    a.rows = desc->rows;
+    a.cols = desc->cols;
+    a.batch = desc->batch;
+    a.np = p.np;
+    a.mp = p.mp;
+    a.parts = p.parts;
+    a.split_gram = p.split_gram;
+    a.split_square = p.split_square;
+    a.split_update = p.split_update;
+    a.in_f32 = desc->dtype == CBW_F32;
+    a.out_f32 = desc->out_dtype == CBW_F32;
+    a.tall = desc->rows > desc->cols;
+    a.a = desc->a;
+    a.b = desc->b;
+    a.c = desc->c;
+    a.eps = desc->eps;
+    a.partial = reinterpret_cast<double*>(ws + p.partial);
+    a.x = reinterpret_cast<float*>(ws + p.x);
+    for (int k = 0; k < 2; ++k) a.planes[k] = reinterpret_cast<_Float16*>(ws + p.planes[k]);
+    a.x_plane = (int64_t)desc->batch * p.np * p.mp;
+    a.gram = reinterpret_cast<_Float16*>(ws + p.gram);
+    a.poly = reinterpret_cast<_Float16*>(ws + p.poly);
+    a.sums = reinterpret_cast<float*>(ws + p.sums);
+    return hip_status(launch_orthogonalize(a, p.tile, desc->steps, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

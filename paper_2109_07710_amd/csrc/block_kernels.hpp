@@ -161,4 +161,41 @@ hipError_t launch_grad_finish(int kind, const double* partial, int npartial, flo
 hipError_t launch_grad_scale(const GradEntry* table, int n, int chunks, int kind, int grid, const double* partial,
                              int npartial, float max_norm, float* norm, hipStream_t s);
 
+// --------------------------------------------------- orthogonalised updates
+
+// Sizes and the workspace of a call.  X is n x m, n <= m, both filled up with
+// zeros to whole tiles.
+struct OrthoPlan {
+    int tile, np, mp;
+    int parts;                              // partial sums of a matrix's norm
+    int split_gram, split_square, split_update;   // parts of a product's reduction
+    int64_t tiles;                          // workgroups of the largest launch
+    size_t partial, x, planes[2], gram, poly, sums, ws_bytes;   // byte offsets
+};
+OrthoPlan ortho_plan(const cbw_ortho_desc* d);
+
+struct OrthoArgs {
+    const void* m;
+    void* o;
+    int64_t in_stride, out_stride;
+    int rows, cols, batch;
+    int np, mp, parts;
+    int split_gram, split_square, split_update;
+    bool in_f32, out_f32, tall;
+    float a, b, c;
+    double eps;
+    double* partial;            // [batch][parts]
+    float* x;                   // [batch][np][mp]
+    _Float16* planes[2];        // X's high parts, then x_plane further its low ones; two sets in turn
+    int64_t x_plane;
+    _Float16 *gram, *poly;      // A and B, [batch][np][np] of high parts, then of low ones
+    float* sums;                // partial sums of split tiles
+};
+struct StepArgs {
+    int from;                   // which of the planes holds X
+    int split;
+    bool last, pair, next_pair;
+};
+hipError_t launch_orthogonalize(const OrthoArgs& a, int tile, int steps, hipStream_t s);
+
 }  // namespace cbw
