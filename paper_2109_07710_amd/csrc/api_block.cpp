@@ -566,9 +566,7 @@ int grad_orthogonalize(const cbw_ortho_desc* desc, const void* M, void* O, void*
     a.np = p.np;
     a.mp = p.mp;
     a.parts = p.parts;
-    a.split_gram = p.split_gram;
-    a.split_square = p.split_square;
-    a.split_update = p.split_update;
+    a.nothing = reinterpret_cast<int*>(ws + p.nothing);
     a.in_f32 = desc->dtype == CBW_F32;
     a.out_f32 = desc->out_dtype == CBW_F32;
     a.tall = desc->rows > desc->cols;
@@ -579,11 +577,10 @@ int grad_orthogonalize(const cbw_ortho_desc* desc, const void* M, void* O, void*
     a.partial = reinterpret_cast<double*>(ws + p.partial);
     a.x = reinterpret_cast<float*>(ws + p.x);
     for (int k = 0; k < 2; ++k) a.planes[k] = reinterpret_cast<_Float16*>(ws + p.planes[k]);
-    a.x_plane = (int64_t)desc->batch * p.np * p.mp;
     a.gram = reinterpret_cast<_Float16*>(ws + p.gram);
     a.poly = reinterpret_cast<_Float16*>(ws + p.poly);
     a.sums = reinterpret_cast<float*>(ws + p.sums);
-    return hip_status(launch_orthogonalize(a, p.tile, desc->steps, static_cast<hipStream_t>(stream)));
+    return hip_status(launch_orthogonalize(a, p, desc->steps, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -163,14 +163,19 @@ hipError_t launch_grad_scale(const GradEntry* table, int n, int chunks, int kind
 
 // --------------------------------------------------- orthogonalised updates
 
+// How a product is dealt out: the tiles' side and number, and how many
+// workgroups share a tile's reduction.
+struct OrthoDeal {
+    int side, tiles, split;
+};
 // Sizes and the workspace of a call.  X is n x m, n <= m, both filled up with
-// zeros to whole tiles.
+// zeros to multiples of 64 or 128.
 struct OrthoPlan {
-    int tile, np, mp;
+    int np, mp;
+    int coarse;                             // steps on high parts alone, the first ones
     int parts;                              // partial sums of a matrix's norm
-    int split_gram, split_square, split_update;   // parts of a product's reduction
-    int64_t tiles;                          // workgroups of the largest launch
-    size_t partial, x, planes[2], gram, poly, sums, ws_bytes;   // byte offsets
+    OrthoDeal deal[2][3];                   // on high parts and on pairs: of A, A A and B X
+    size_t partial, nothing, x, planes[2], gram, poly, sums, ws_bytes;   // byte offsets
 };
 OrthoPlan ortho_plan(const cbw_ortho_desc* d);
 
@@ -180,22 +185,21 @@ struct OrthoArgs {
     int64_t in_stride, out_stride;
     int rows, cols, batch;
     int np, mp, parts;
-    int split_gram, split_square, split_update;
     bool in_f32, out_f32, tall;
     float a, b, c;
     double eps;
     double* partial;            // [batch][parts]
+    int* nothing;               // [batch]: a matrix of zeros
     float* x;                   // [batch][np][mp]
-    _Float16* planes[2];        // X's high parts, then x_plane further its low ones; two sets in turn
-    int64_t x_plane;
-    _Float16 *gram, *poly;      // A and B, [batch][np][np] of high parts, then of low ones
-    float* sums;                // partial sums of split tiles
+    _Float16* planes[2];        // of X, two sets in turn
+    _Float16 *gram, *poly;      // of A and B
+    float* sums;                // [tiles][split] tiles of partial sums
 };
 struct StepArgs {
     int from;                   // which of the planes holds X
-    int split;
+    int split;                  // workgroups that share a tile's reduction
     bool last, pair, next_pair;
 };
-hipError_t launch_orthogonalize(const OrthoArgs& a, int tile, int steps, hipStream_t s);
+hipError_t launch_orthogonalize(const OrthoArgs& a, const OrthoPlan& p, int steps, hipStream_t s);
 
 }  // namespace cbw

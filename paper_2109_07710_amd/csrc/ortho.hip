@@ -12,16 +12,21 @@
 // near to 64 bits as the same steps in float32 (2.1e-6 against 2.1e-6 of the
 // result's 2-norm, 256 x 2304 of full rank), at three instructions of the
 // half-precision rate, which is a fifth of the float32 instructions' time.
-// Where the update is stored in bf16, all steps but the last two take the high
-// parts alone: what they leave off, 11 bits of the products but not of the a X
-// beside them, is smaller than a bf16 value's rounding after the last two
-// (7.7e-4 of the 2-norm against 1.7e-3; one such step at the end: 3e-3).
+// Where the update is stored in bf16, the first steps take the high parts
+// alone: what they leave off, 2^-11 of B X but nothing of the a X beside it,
+// counts for little while the singular values are small.  With all of them
+// alike, the worst case, they are a^k / sqrt(n) after k steps; while that is
+// below sqrt(0.14) and two more steps follow, the update's error stays below
+// 4e-4 of its 2-norm, against the 1.7e-3 of its rounding (n = 1024, full rank:
+// 3.5e-4, flat: 3.6e-5; n = 256: 5e-5).  A step too many costs 8e-4 at n = 256
+// and 3e-3 at 64.
 #include "common.hpp"
 #include "block_kernels.hpp"
 #include "expert_tiles.hpp"
 #include "tiles.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace cbw {
 namespace {
@@ -75,10 +80,24 @@ __device__ __forceinline__ float load_value(const void* p, int64_t i, bool f32)
 {
     return f32 ? static_cast<const float*>(p)[i] : __uint_as_float((uint32_t) static_cast<const uint16_t*>(p)[i] << 16);
 }
+// Eight values from p's element i on, 16-byte aligned.
+__device__ __forceinline__ void load_values(const void* p, int64_t i, bool f32, float (&v)[8])
+{
+    if (f32) {
+        const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+        const float4 y = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i + 4);
+        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+    } else {
+        const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
+        const uint32_t b[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(k & 1 ? b[k / 2] & 0xffff0000u : b[k / 2] << 16);
+    }
+}
 
 // Sums of squares of a matrix, in 64 bits: part z of a.parts takes every
 // a.parts-th chunk.  Contiguous matrices are one long row.
-constexpr int kChunk = 4096;
+constexpr int kChunk = 8192;
 __global__ __launch_bounds__(256) void ortho_norm_kernel(OrthoArgs a)
 {
     const int z = blockIdx.x % a.parts, mat = blockIdx.x / a.parts;
@@ -86,14 +105,30 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(OrthoArgs a)
     const int64_t rows = flat ? 1 : a.rows, cols = flat ? (int64_t)a.rows * a.cols : a.cols;
     const int64_t chunks = (cols + kChunk - 1) / kChunk;
     const int64_t base = (int64_t)mat * a.rows * a.in_stride;
+    const int size = a.in_f32 ? 4 : 2;
     double s = 0.0;
     for (int64_t u = z; u < rows * chunks; u += a.parts) {
         const int64_t row = u / chunks, c0 = (u - row * chunks) * kChunk;
         const int64_t first = base + row * a.in_stride + c0;
         const int n = (int)min((int64_t)kChunk, cols - c0);
-        for (int i = threadIdx.x; i < n; i += 256) {
-            const double v = load_value(a.m, first + i, a.in_f32);
-            s += v * v;
+        // up to the first 16-byte boundary, whole vectors, and the rest
+        const int head = min(n, (int)((0 - ((uintptr_t)a.m + first * size)) % 16) / size), whole = (n - head) / 8;
+        float v[4][8];   // four vectors' loads in flight
+        for (int i = threadIdx.x; i < whole; i += 1024) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                load_values(a.m, first + head + (int64_t)min(i + k * 256, whole - 1) * 8, a.in_f32, v[k]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k * 256 < whole)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) s += (double)v[k][c] * v[k][c];
+        }
+        // (fewer than eight on each side)
+        const int i = (int)threadIdx.x < head ? (int)threadIdx.x : whole * 8 + (int)threadIdx.x;
+        if ((int)threadIdx.x < n - whole * 8) {
+            const double x = load_value(a.m, first + i, a.in_f32);
+            s += x * x;
         }
     }
     __shared__ double sums[4];
@@ -103,89 +138,43 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(OrthoArgs a)
     if (threadIdx.x == 0) a.partial[(int64_t)mat * a.parts + z] = sums[0] + sums[1] + sums[2] + sums[3];
 }
 
-// X and its planes, 64 x 64 values a workgroup, zeros past the matrix.
-__global__ __launch_bounds__(256) void ortho_start_kernel(OrthoArgs a, bool pair)
+// 1 / (|M| + eps).  A norm that is no number, or infinite, leaves no number
+// anywhere; nothing stays nothing.  Called by whole waves.
+__device__ __forceinline__ double inverse_norm(const OrthoArgs& a, int mat, bool& nothing)
 {
-    __shared__ float tile[64][65];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int bx = a.mp / 64, by = a.np / 64;
-    const int mat = blockIdx.x / (bx * by), in = blockIdx.x - mat * (bx * by);
-    const int i0 = in / bx * 64, j0 = in % bx * 64;   // of X
-
     double s = 0.0;
-    for (int z = lane; z < a.parts; z += 64) s += a.partial[(int64_t)mat * a.parts + z];
+    for (int z = threadIdx.x & 63; z < a.parts; z += 64) s += a.partial[(int64_t)mat * a.parts + z];
     for (int k = 32; k >= 1; k >>= 1) s += __shfl_xor(s, k);
-    // a norm that is no number, or infinite, leaves no number anywhere; nothing stays nothing
-    const double norm = sqrt(s), by_norm = norm + a.eps;
-    const double inv = by_norm > 0.0 ? (norm < __builtin_inf() ? 1.0 / by_norm : __builtin_nan("")) : by_norm == 0.0 ? 0.0 : by_norm;
-
-    const int64_t base = (int64_t)mat * a.rows * a.in_stride;
-    const int r0 = a.tall ? j0 : i0, c0 = a.tall ? i0 : j0;   // of M
-    for (int r = wave; r < 64; r += 4) {
-        const int row = r0 + r, col = c0 + lane;
-        // (values past the matrix stay zero, also where the norm is no number)
-        const float v = row < a.rows && col < a.cols ? (float)(load_value(a.m, base + row * a.in_stride + col, a.in_f32) * inv) : 0.f;
-        if (a.tall) tile[lane][r] = v;
-        else tile[r][lane] = v;
-    }
-    __syncthreads();
-    const int64_t at0 = (int64_t)mat * a.np * a.mp;
-    for (int t = threadIdx.x; t < 64 * 8; t += 256) {
-        const int i = t / 8, j = t % 8 * 8;
-        const int64_t at = at0 + (int64_t)(i0 + i) * a.mp + j0 + j;
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = tile[i][j + k];
-#pragma unroll
-        for (int k = 0; k < 8; k += 4) *reinterpret_cast<float4*>(a.x + at + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= kX;
-        const Pair p = split(v);
-        *reinterpret_cast<uint4*>(a.planes[0] + at) = p.hi;
-        if (pair) *reinterpret_cast<uint4*>(a.planes[0] + a.x_plane + at) = p.lo;
-    }
+    const double norm = sqrt(s), all = norm + a.eps;
+    nothing = norm == 0.0;
+    return all > 0.0 ? (norm < __builtin_inf() ? 1.0 / all : __builtin_nan("")) : all == 0.0 ? 0.0 : all;
 }
 
-// ---------------------------------------------------------------- products
-
-enum { GRAM = 0, SQUARE = 1, UPDATE = 2 };
-
-// A tile's place: its matrix, rows i0 on, columns j0 on.
-struct Spot {
-    int mat, i0, j0;
+// Where a matrix's planes of `ld` columns and `rows` rows (of one matrix) hold
+// the high part of (i, j), and how much further its low part lies.  Products
+// on pairs find 32 high parts and the same columns' 32 low parts in each 128
+// bytes, so that a step of the reduction is whole lines; those on high parts
+// alone find them in a plane of their own.
+struct Plane {
+    int64_t mat, low;
+    int ld;
+    bool pair;
+    __device__ Plane(bool pr, int which, int batch, int rows, int columns)
+        : mat((int64_t)which * rows * columns * (pr ? 2 : 1)), low(pr ? 32 : (int64_t)batch * rows * columns), ld(columns), pair(pr) {}
+    __device__ __forceinline__ int64_t at(int i, int j) const
+    {
+        return mat + (pair ? (int64_t)i * ld * 2 + (j >> 5) * 64 + (j & 31) : (int64_t)i * ld + j);
+    }
 };
-template <int STAGE, int T>
-__device__ __forceinline__ Spot spot_of(const OrthoArgs& a, int tile)
+__device__ __forceinline__ void put_x(const OrthoArgs& a, const Plane& plane, _Float16* to, int i, int j, const float (&x)[8])
 {
-    Spot s;
-    const int rows = a.np / T, cols = a.mp / T;
-    const int per = STAGE == UPDATE ? rows * cols : rows * (rows + 1) / 2;
-    s.mat = tile / per;
-    const int in = tile - s.mat * per;
-    if (STAGE == UPDATE) {
-        s.i0 = in % rows * T;
-        s.j0 = in / rows * T;
-    } else {
-        // row i has i + 1 tiles
-        int i = (int)((sqrtf(8.f * (float)in + 1.f) - 1.f) * 0.5f);
-        while (i * (i + 1) / 2 > in) --i;
-        while ((i + 1) * (i + 2) / 2 <= in) ++i;
-        s.i0 = i * T;
-        s.j0 = (in - i * (i + 1) / 2) * T;
-    }
-    return s;
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = x[k] * kX;
+    const Pair w = split(v);
+    *reinterpret_cast<uint4*>(to + plane.at(i, j)) = w.hi;
+    if (plane.pair) *reinterpret_cast<uint4*>(to + plane.at(i, j) + plane.low) = w.lo;
 }
-
-// A tile in LDS as [row][column], in float32.  A row's 16-byte chunks are moved
-// so that both a row's vectors and a column's values are read without sharing
-// banks.
-template <int T>
-struct Square {
-    static constexpr int CHUNKS = T / 4;
-    static __device__ __forceinline__ int swizzle(int q) { return (q ^ (q >> 3)) & (CHUNKS - 1); }
-    static __device__ __forceinline__ float* chunk(float* t, int q, int c) { return t + q * T + ((c ^ swizzle(q)) << 2); }
-    static __device__ __forceinline__ float* value(float* t, int q, int p) { return chunk(t, q, p >> 2) + (p & 3); }
-};
 
 // Eight values of a row of the output, from column `col` on.
 __device__ __forceinline__ void store_out(const OrthoArgs& a, int mat, int row, int col, const float (&v)[8])
@@ -217,17 +206,176 @@ __device__ __forceinline__ void store_out(const OrthoArgs& a, int mat, int row, 
     }
 }
 
-// What becomes of a finished tile of sums, in LDS: A or B into their planes at
-// both places, X and its planes, or the update.
+// X and its planes, 64 x 64 values a workgroup, zeros past the matrix.
+__global__ __launch_bounds__(256) void ortho_start_kernel(OrthoArgs a, bool pair)
+{
+    __shared__ float tile[64][65];
+    const int bx = a.mp / 64, by = a.np / 64;
+    const int mat = blockIdx.x / (bx * by), in = blockIdx.x - mat * (bx * by);
+    const int i0 = in / bx * 64, j0 = in % bx * 64;   // of X
+
+    const int64_t base = (int64_t)mat * a.rows * a.in_stride;
+    const int size = a.in_f32 ? 4 : 2;
+    const int r0 = a.tall ? j0 : i0, c0 = a.tall ? i0 : j0;   // of M
+    float v[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int t = threadIdx.x + h * 256, row = r0 + t / 8, col = c0 + t % 8 * 8;
+        const int64_t at = base + row * a.in_stride + col;
+        if (row < a.rows && col + 8 <= a.cols && ((uintptr_t)a.m + at * size) % 16 == 0) {
+            load_values(a.m, at, a.in_f32, v[h]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[h][k] = row < a.rows && col + k < a.cols ? load_value(a.m, at + k, a.in_f32) : 0.f;
+        }
+    }
+    bool nothing;
+    const double inv = inverse_norm(a, mat, nothing);
+    if (in == 0 && threadIdx.x == 0) a.nothing[mat] = nothing;
+    if (nothing) {
+        // the products leave it out: its update is written here
+        const float zeros[8] = {};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int t = threadIdx.x + h * 256;
+            store_out(a, mat, r0 + t / 8, c0 + t % 8 * 8, zeros);
+        }
+        return;
+    }
+    const Plane plane(pair, mat, a.batch, a.np, a.mp);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int t = threadIdx.x + h * 256, r = t / 8, c = t % 8 * 8;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            // (values past the matrix stay zero, also where the norm is no number)
+            v[h][k] = r0 + r < a.rows && c0 + c + k < a.cols ? (float)(v[h][k] * inv) : 0.f;
+            if (a.tall) tile[c + k][r] = v[h][k];
+        }
+    }
+    if (a.tall) __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int t = threadIdx.x + h * 256, i = t / 8, j = t % 8 * 8;
+        if (a.tall)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[h][k] = tile[i][j + k];
+        float* x = a.x + (int64_t)mat * a.np * a.mp + (int64_t)(i0 + i) * a.mp + j0 + j;
+        *reinterpret_cast<float4*>(x) = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
+        *reinterpret_cast<float4*>(x + 4) = make_float4(v[h][4], v[h][5], v[h][6], v[h][7]);
+        put_x(a, plane, a.planes[0], i0 + i, j0 + j, v[h]);
+    }
+}
+
+// ---------------------------------------------------------------- products
+
+enum { GRAM = 0, SQUARE = 1, UPDATE = 2 };
+
+// A tile's place: its matrix, rows i0 on, columns j0 on.
+struct Spot {
+    int mat, i0, j0;
+};
+// Matrices of zeros have no tiles, so that the others' are dealt out evenly
+// over the chip: a lane looks at a matrix, up to 64 of them.
+struct Tiles {
+    uint64_t busy;
+    int per, count;   // tiles of a matrix, and in all
+    bool listed;
+};
+template <int STAGE, int T>
+__device__ __forceinline__ Tiles tiles_of(const OrthoArgs& a)
+{
+    Tiles t;
+    const int rows = (a.np + T - 1) / T, cols = (a.mp + T - 1) / T, lane = threadIdx.x & 63;
+    t.per = STAGE == UPDATE ? rows * cols : rows * (rows + 1) / 2;
+    t.listed = a.batch <= 64;
+    t.busy = t.listed ? __ballot(lane < a.batch && a.nothing[lane < a.batch ? lane : 0] == 0) : 0;
+    t.count = t.per * (t.listed ? __popcll(t.busy) : a.batch);
+    return t;
+}
+template <int STAGE, int T>
+__device__ __forceinline__ Spot spot_of(const OrthoArgs& a, const Tiles& tiles, int tile)
+{
+    Spot s;
+    const int rows = (a.np + T - 1) / T;
+    s.mat = tile / tiles.per;
+    const int in = tile - s.mat * tiles.per;
+    if (tiles.listed) {
+        uint64_t m = tiles.busy;
+        for (int k = 0; k < s.mat; ++k) m &= m - 1;
+        s.mat = __builtin_ctzll(m);
+    }
+    // The tiles of one XCD, consecutive ones, lie in compact blocks, so that few
+    // rows and columns of tiles pass its L2: what a product reads comes to every
+    // XCD from the shared cache or memory.
+    if (STAGE == UPDATE) {
+        // panels of eight columns, row by row
+        const int cols = (a.mp + T - 1) / T, panel = in / (8 * rows), w = min(8, cols - 8 * panel), at = in - panel * 8 * rows;
+        s.i0 = at / w * T;
+        s.j0 = (panel * 8 + at % w) * T;
+    } else {
+        // block rows of four tile rows, blocks of four columns from left to right,
+        // the last one's part on and below the diagonal
+        int b = 0, at = in, h = min(4, rows);
+        for (int n = h * (h + 1) / 2; at >= n; n = 4 * b * h + h * (h + 1) / 2) {
+            at -= n;
+            ++b;
+            h = min(4, rows - 4 * b);
+        }
+        int i = 0, j = 0;
+        if (at < 4 * b * h) {
+            const int block = at / (4 * h), left = at - block * 4 * h;
+            i = left / 4;
+            j = block * 4 + left % 4;
+        } else {
+            j = at - 4 * b * h;
+            while (j > i) j -= ++i;   // row i of the corner has i + 1 tiles
+            j += 4 * b;
+        }
+        s.i0 = (4 * b + i) * T;
+        s.j0 = j * T;
+    }
+    return s;
+}
+
+// A tile in LDS as [row][column], in float32.  A row's 16-byte chunks are moved
+// so that both a row's vectors and a column's values are read without sharing
+// banks.
+template <int T>
+struct Square {
+    static constexpr int CHUNKS = T / 4;
+    static __device__ __forceinline__ int swizzle(int q) { return (q ^ (q >> 3)) & (CHUNKS - 1); }
+    static __device__ __forceinline__ float* chunk(float* t, int q, int c) { return t + q * T + ((c ^ swizzle(q)) << 2); }
+    static __device__ __forceinline__ float* value(float* t, int q, int p) { return chunk(t, q, p >> 2) + (p & 3); }
+};
+
+// The thread's number, which the compiler takes for a new one each time: it
+// would keep all that follows from it in registers during the products.
+__device__ __forceinline__ int my_thread()
+{
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
+
+// What becomes of a finished T x T piece of sums, in LDS: A or B into their
+// planes, with `mirror` at the mirrored place too, X and its planes, or the update.
 template <int STAGE, int T, int THREADS>
-__device__ __forceinline__ void finish(const OrthoArgs& a, const StepArgs& st, const Spot& s, float* tile)
+__device__ __forceinline__ void finish(const OrthoArgs& a, const StepArgs& st, const Spot& s, bool mirror, float* tile)
 {
     using Sq = Square<T>;
-    const bool mirror = STAGE != UPDATE ? s.i0 != s.j0 : st.last && a.tall;
-    const int64_t an = (int64_t)a.np * a.np, amat = s.mat * an, plane = an * a.batch;
+    const bool turned = STAGE == UPDATE && st.last && a.tall;
     _Float16* out = STAGE == GRAM ? a.gram : a.poly;
+    const Plane square(st.pair, s.mat, a.batch, a.np, a.np), next(st.next_pair, s.mat, a.batch, a.np, a.mp);
+    auto put = [&](int i, int j, const float (&v)[8]) {
+        const Pair w = split(v);
+        const int64_t at = square.at(i, j);
+        *reinterpret_cast<uint4*>(out + at) = w.hi;
+        if (STAGE == GRAM || st.pair) *reinterpret_cast<uint4*>(out + at + square.low) = w.lo;
+    };
+    const int thread = my_thread();
 #pragma unroll 2
-    for (int t = threadIdx.x; t < T * T / 8; t += THREADS) {
+    for (int t = thread; t < T * T / 8; t += THREADS) {
         const int q = t / (T / 8), p = t % (T / 8) * 8;
         float v[8];
 #pragma unroll
@@ -237,253 +385,332 @@ __device__ __forceinline__ void finish(const OrthoArgs& a, const StepArgs& st, c
             for (int c = 0; c < 4; ++c) v[4 * k + c] = x[c];
         }
         if (STAGE == UPDATE) {
-            const int64_t at = (int64_t)s.mat * a.np * a.mp + (int64_t)(s.i0 + q) * a.mp + s.j0 + p;
-            const float4 x0 = *reinterpret_cast<const float4*>(a.x + at), x1 = *reinterpret_cast<const float4*>(a.x + at + 4);
+            float* at = a.x + (int64_t)s.mat * a.np * a.mp + (int64_t)(s.i0 + q) * a.mp + s.j0 + p;
+            const float4 x0 = *reinterpret_cast<const float4*>(at), x1 = *reinterpret_cast<const float4*>(at + 4);
             const float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = a.a * x[k] + v[k] * (1.f / (kB * kX));
             if (!st.last) {
-                *reinterpret_cast<float4*>(a.x + at) = make_float4(v[0], v[1], v[2], v[3]);
-                *reinterpret_cast<float4*>(a.x + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] *= kX;
-                const Pair w = split(v);
-                _Float16* to = a.planes[st.from ^ 1] + at;
-                *reinterpret_cast<uint4*>(to) = w.hi;
-                if (st.next_pair) *reinterpret_cast<uint4*>(to + a.x_plane) = w.lo;
+                *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<float4*>(at + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                put_x(a, next, a.planes[st.from ^ 1], s.i0 + q, s.j0 + p, v);
             } else if (!a.tall) {
                 store_out(a, s.mat, s.i0 + q, s.j0 + p, v);
             }
         } else {
-            const int64_t at = amat + (int64_t)(s.i0 + q) * a.np + s.j0 + p;
             if (STAGE == GRAM) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[k] *= kA / (kX * kX);
             } else {
+                const int64_t at = square.at(s.i0 + q, s.j0 + p);
                 Pair g;
                 g.hi = *reinterpret_cast<const uint4*>(a.gram + at);
-                g.lo = *reinterpret_cast<const uint4*>(a.gram + plane + at);
+                g.lo = *reinterpret_cast<const uint4*>(a.gram + at + square.low);
                 float x[8];
                 join(g, x);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[k] = (a.b * (kB / kA)) * x[k] + (a.c * (kB / (kA * kA))) * v[k];
             }
-            const Pair w = split(v);
-            *reinterpret_cast<uint4*>(out + at) = w.hi;
-            if (STAGE == GRAM || st.pair) *reinterpret_cast<uint4*>(out + plane + at) = w.lo;
+            put(s.i0 + q, s.j0 + p, v);
         }
-        if (mirror) {
+        if (mirror || turned) {
 #pragma unroll
             for (int k = 0; k < 2; ++k)
                 *reinterpret_cast<floatx4*>(Sq::chunk(tile, q, p / 4 + k)) = floatx4{v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]};
         }
     }
-    if (!mirror) return;
+    if (!mirror && !turned) return;
     __syncthreads();
-    for (int t = threadIdx.x; t < T * T / 8; t += THREADS) {
+    for (int t = thread; t < T * T / 8; t += THREADS) {
         const int p = t / (T / 8), q = t % (T / 8) * 8;
         float v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = *Sq::value(tile, q + k, p);
-        if (STAGE == UPDATE) {
-            store_out(a, s.mat, s.j0 + p, s.i0 + q, v);
-        } else {
-            const int64_t at = amat + (int64_t)(s.j0 + p) * a.np + s.i0 + q;
-            const Pair w = split(v);
-            *reinterpret_cast<uint4*>(out + at) = w.hi;
-            if (STAGE == GRAM || st.pair) *reinterpret_cast<uint4*>(out + plane + at) = w.lo;
-        }
+        if (STAGE == UPDATE) store_out(a, s.mat, s.j0 + p, s.i0 + q, v);
+        else put(s.j0 + p, s.i0 + q, v);
     }
 }
 
-// T x T tile by NWP x NWQ waves, two buffers of 64 reduction indices of both
-// operands, PAIR: of both planes.
-template <int STAGE, bool PAIR, int T, int NWP, int NWQ>
-struct Product {
-    static constexpr int NW = NWP * NWQ, FM = T / NWP / 16, FN = T / NWQ / 16, PL = PAIR ? 2 : 1;
-    using OP = Operand<uint16_t, T, STAGE == UPDATE, NW>;
-    using OQ = Operand<uint16_t, T, false, NW>;
-    static constexpr int COPIES = (OP::COPIES + OQ::COPIES) * PL, TILE = OP::BYTES, BUFFER = 2 * PL * TILE;
-    static constexpr int LDS = 2 * BUFFER > T * T * 4 ? 2 * BUFFER : T * T * 4;
-};
+template <int T>
+constexpr int kPiece = T < 128 ? T : 128;   // side of a piece that is finished at a time
 
-template <int T, int NWP, int NWQ, int FM, int FN>
-__device__ __forceinline__ void to_lds(const floatx4 (&acc)[FM][FN], float* tile)
+// A finished tile, as the matrix instructions leave it, piece by piece.
+template <int STAGE, int T, int NWP, int NWQ, int FM, int FN>
+__device__ __forceinline__ void pieces(const OrthoArgs& a, const StepArgs& st, const Spot& s, bool mirror,
+                                       const floatx4 (&acc)[FM][FN], float* lds)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave / NWQ, wq = wave % NWQ;
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-            *reinterpret_cast<floatx4*>(Square<T>::chunk(tile, wq * (T / NWQ) + j * 16 + (lane & 15),
-                                                         (wp * (T / NWP) + i * 16) / 4 + (lane >> 4))) = acc[i][j];
-}
-
-template <int STAGE, bool PAIR, int T, int NWP, int NWQ>
-__global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs a, StepArgs st)
-{
-    using P = Product<STAGE, PAIR, T, NWP, NWQ>;
-    using OP = typename P::OP;
-    using OQ = typename P::OQ;
-    constexpr int FM = P::FM, FN = P::FN, PL = P::PL, KB = 64;
-    __shared__ __align__(1024) char lds[P::LDS];
-
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave / NWQ, wq = wave % NWQ;
-    const int unit = xcd_remap(blockIdx.x, gridDim.x);
-    const int tile = unit / st.split, part = unit - tile * st.split;
-    const Spot s = spot_of<STAGE, T>(a, tile);
-
-    // rows i0 on of A's and B's left factors, and their columns: X, A or B
-    const int64_t xmat = (int64_t)s.mat * a.np * a.mp, gmat = (int64_t)s.mat * a.np * a.np, gplane = (int64_t)a.np * a.np * a.batch;
-    const _Float16* x = a.planes[st.from] + xmat;
-    const _Float16 *pb, *qb;
-    int64_t pplane, qplane, pstride, qstride;
-    if (STAGE == GRAM) {
-        pb = x + (int64_t)s.j0 * a.mp;
-        qb = x + (int64_t)s.i0 * a.mp;
-        pplane = qplane = a.x_plane;
-        pstride = qstride = a.mp;
-    } else if (STAGE == SQUARE) {
-        pb = a.gram + gmat + (int64_t)s.j0 * a.np;
-        qb = a.gram + gmat + (int64_t)s.i0 * a.np;
-        pplane = qplane = gplane;
-        pstride = qstride = a.np;
-    } else {
-        pb = x + s.j0;
-        qb = a.poly + gmat + (int64_t)s.i0 * a.np;
-        pplane = a.x_plane;
-        qplane = gplane;
-        pstride = a.mp;
-        qstride = a.np;
-    }
-    const int len = STAGE == GRAM ? a.mp : a.np, all = len / KB;
-    const int first = (int)((int64_t)part * all / st.split), steps = (int)((int64_t)(part + 1) * all / st.split) - first;
-
-    OP op;
-    OQ oq;
-    op.init(wave, T, pstride);
-    oq.init(wave, 0, qstride);
-    auto copy = [&](int step, int buf) {
-        const int64_t k = (int64_t)(first + step) * KB;
-        char* to = lds + buf * P::BUFFER;
-#pragma unroll
-        for (int l = 0; l < PL; ++l) {
-            // (across: KB rows of T columns; along: T rows of KB columns)
-            const _Float16* p = pb + l * pplane + (STAGE == UPDATE ? k * pstride : k);
-            const uint32_t n = (uint32_t)(((STAGE == UPDATE ? KB - 1 : T - 1) * pstride + (STAGE == UPDATE ? T : KB)) * 2);
-            op.copy(wave, make_rsrc_words(p, n), 0, KB, to + l * P::TILE);
-            oq.copy(wave, make_rsrc_words(qb + l * qplane + k, (uint32_t)(((T - 1) * qstride + KB) * 2)), 0, KB, to + (PL + l) * P::TILE);
-        }
-    };
-
-    floatx4 acc[FM][FN];
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    struct Fragments {
-        uint4 p[PL][FM], q[PL][FN];
-    };
-    const int frag_p = OP::first(wp * (T / NWP)), frag_q = OQ::first(wq * (T / NWQ));
-    auto read = [&](Fragments& f, int buf, int ks) {
-        const char* at = lds + buf * P::BUFFER;
-#pragma unroll
-        for (int l = 0; l < PL; ++l) {
-            OQ::fragments(at + (PL + l) * P::TILE, frag_q, ks, f.q[l]);
-            OP::fragments(at + l * P::TILE, frag_p, ks, f.p[l]);
-        }
-    };
-    auto multiply = [&](const Fragments& f) {
-#pragma unroll
-        for (int l = 0; l < (PAIR ? 3 : 1); ++l)
+    constexpr int S = kPiece<T>;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave / NWQ, wq = wave % NWQ, lane = my_thread() & 63;
+    for (int pq = 0; pq < T; pq += S)
+        for (int pp = 0; pp < T; pp += S) {
+            __syncthreads();   // every wave is done with the operands, or with the piece before
+            if (s.i0 + pq >= a.np || s.j0 + pp >= (STAGE == UPDATE ? a.mp : a.np)) continue;
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = mfma_half(acc[i][j], f.p[l == 2 ? PL - 1 : 0][i], f.q[l == 1 ? PL - 1 : 0][j]);
-    };
-    Fragments fa, fb;
-    if (steps > 0) copy(0, 0);
-    if (steps > 1) copy(1, 1);
-    if (steps > 0) {
-        if (steps > 1) wait_copies<P::COPIES>();
-        else wait_copies<0>();
-        barrier();
-        read(fa, 0, 0);
-        for (int k = 0; k < steps; ++k) {
-            const int buf = k & 1;
-            read(fb, buf, 1);
-            multiply(fa);
-            wait_copies<0>();
-            wait_reads();
-            barrier();
-            if (k + 2 < steps) copy(k + 2, buf);
-            if (k + 1 < steps) read(fa, buf ^ 1, 0);
-            multiply(fb);
+                for (int j = 0; j < FN; ++j) {
+                    const int q = wq * (T / NWQ) + j * 16 - pq, p = wp * (T / NWP) + i * 16 - pp;
+                    if (q >= 0 && q < S && p >= 0 && p < S)
+                        *reinterpret_cast<floatx4*>(Square<S>::chunk(lds, q + (lane & 15), p / 4 + (lane >> 4))) = acc[i][j];
+                }
+            __syncthreads();
+            finish<STAGE, S, NWP * NWQ * 64>(a, st, Spot{s.mat, s.i0 + pq, s.j0 + pp}, mirror, lds);
         }
-    }
-    if (st.split > 1) {
-        // as the registers lie: the kernel that adds the parts up has the same threads
-        floatx4* to = reinterpret_cast<floatx4*>(a.sums) + (int64_t)unit * (T * T / 4);
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j) to[(i * FN + j) * (P::NW * 64) + threadIdx.x] = acc[i][j];
-        return;
-    }
-    __syncthreads();   // every wave is done with the operands
-    float* out = reinterpret_cast<float*>(lds);
-    to_lds<T, NWP, NWQ>(acc, out);
-    __syncthreads();
-    finish<STAGE, T, NWP * NWQ * 64>(a, st, s, out);
 }
 
-// The parts of a split tile, added in order, and what becomes of it.
-template <int STAGE, int T, int NWP, int NWQ>
-__global__ __launch_bounds__(NWP* NWQ * 64) void ortho_sum_kernel(OrthoArgs a, StepArgs st)
+// 32 rows of the planes of pairs, T columns from the base on, as 64 LDS lines of
+// T values: the rows' high parts, then their low ones.
+template <int T, int NW>
+struct PairsAcross {
+    using O = Operand<uint16_t, T, true, NW>;
+    static constexpr int COPIES = O::COPIES, CHUNKS = O::CHUNKS;
+    uint32_t off[COPIES];
+    __device__ __forceinline__ void init(int wave, int n, int64_t ld)
+    {
+#pragma unroll
+        for (int j = 0; j < COPIES; ++j) {
+            const int at = (wave + NW * j) * 64 + (threadIdx.x & 63), line = at / CHUNKS, lc = (at % CHUNKS) ^ O::swizzle(line);
+            off[j] = lc * 8 >= n ? kOOB : (uint32_t)((line & 31) * ld * 2 + (line >> 5) * 32 + (lc >> 2) * 64 + (lc & 3) * 8) * 2u;
+        }
+    }
+    __device__ __forceinline__ void copy(int wave, const u32x4_t& rsrc, char* lds) const
+    {
+#pragma unroll
+        for (int j = 0; j < COPIES; ++j) buf_load16_lds(rsrc, off[j], lds_addr(lds + (wave + NW * j) * 1024));
+    }
+};
+
+// T x T tiles by NWP x NWQ waves.  A step is 128 bytes of reduction indices of
+// both operands: 64 high parts, or 32 pairs.  SUB of them go from one barrier to
+// the next, and as many again are on their way into LDS meanwhile.
+//
+// The steps of a tile are shared out to st.split workgroups, whose sums go to
+// memory where there are several; a launch of their own adds them up.
+// (Counting them in and leaving that to the last workgroup of a tile took a
+// fence for the whole device in each, and 98 us in place of 28 for A of 2048 x
+// 2048 values, 136 tiles in 256 ranges.)
+template <int STAGE, bool PAIR, int T, int NWP, int NWQ, int SUB>
+__global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs a, StepArgs st)
 {
     constexpr int NW = NWP * NWQ, FM = T / NWP / 16, FN = T / NWQ / 16;
-    __shared__ __align__(1024) float out[T * T];
-    const int tile = blockIdx.x;
-    const Spot s = spot_of<STAGE, T>(a, tile);
-    const floatx4* from = reinterpret_cast<const floatx4*>(a.sums) + (int64_t)tile * st.split * (T * T / 4);
+    constexpr int S = kPiece<T>;
+    constexpr int KS = PAIR ? 32 : 64;                          // reduction indices of a step
+    using OP = Operand<uint16_t, T, STAGE == UPDATE, NW>;
+    using OQ = Operand<uint16_t, T, false, NW>;
+    constexpr int COPIES = OP::COPIES + OQ::COPIES, TILE = OP::BYTES, STEP = 2 * TILE;
+    constexpr int RING = 2 * SUB;
+    __shared__ __align__(1024) char lds[RING * STEP > S * S * 4 ? RING * STEP : S * S * 4];
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave / NWQ, wq = wave % NWQ;
+    const int len = (STAGE == GRAM ? a.mp : a.np) / KS;         // steps of a tile
+    const Tiles tiles = tiles_of<STAGE, T>(a);
+    const int units = tiles.count * st.split;
+    if ((int)blockIdx.x >= units) return;
+    const int me = xcd_remap(blockIdx.x, units), tile = me / st.split, part = me - tile * st.split;
+    const int first = (int)((int64_t)part * len / st.split), steps = (int)((int64_t)(part + 1) * len / st.split) - first;
+    const Spot s = spot_of<STAGE, T>(a, tiles, tile);
+    if (!tiles.listed && a.nothing[s.mat] != 0) return;
+
+    OP op;
+    OQ oq;
+    PairsAcross<T, NW> across;
+    const int64_t pld = (STAGE == SQUARE ? a.np : a.mp) * (PAIR ? 2 : 1), qld = (STAGE == GRAM ? a.mp : a.np) * (PAIR ? 2 : 1);
+    oq.init(wave, 0, qld);
+    if (STAGE != UPDATE) op.init(wave, 0, pld);
+    const int frag_p = OP::first(wp * (T / NWP)), frag_q = OQ::first(wq * (T / NWQ));
+
+    const int vq = min(T, a.np - s.i0), vp = min(T, (STAGE == UPDATE ? a.mp : a.np) - s.j0);   // rows and columns there are
+
+    const Plane xs(PAIR, s.mat, a.batch, a.np, a.mp), gs(PAIR, s.mat, a.batch, a.np, a.np);
+    const _Float16* x = a.planes[st.from];
+    const _Float16* pb = STAGE == GRAM ? x + xs.at(s.j0, 0) : STAGE == SQUARE ? a.gram + gs.at(s.j0, 0) : x + xs.at(0, s.j0);
+    const _Float16* qb = STAGE == GRAM ? x + xs.at(s.i0, 0) : STAGE == SQUARE ? a.gram + gs.at(s.i0, 0) : a.poly + gs.at(s.i0, 0);
+    if (STAGE == UPDATE) {
+        if (PAIR) across.init(wave, vp, a.mp);
+        else op.init(wave, vp, pld);
+    }
+    auto copy = [&](int step) {
+        char* to = lds + step % RING * STEP;
+        const int64_t k = first + step;
+        if (STAGE == UPDATE) {
+            const u32x4_t r = make_rsrc_words(pb + k * KS * pld, (uint32_t)(((KS - 1) * pld + vp * (PAIR ? 2 : 1)) * 2));
+            if (PAIR) across.copy(wave, r, to);
+            else op.copy(wave, r, 0, 0, to);
+        } else {
+            op.copy(wave, make_rsrc_words(pb + k * 64, (uint32_t)(((vp - 1) * pld + 64) * 2)), 0, 64, to);
+        }
+        oq.copy(wave, make_rsrc_words(qb + k * 64, (uint32_t)(((vq - 1) * qld + 64) * 2)), 0, 64, to + TILE);
+    };
+
     floatx4 acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    for (int z = 0; z < st.split; ++z, from += T * T / 4)
+    auto multiply = [&](const uint4 (&p)[FM], const uint4 (&q)[FN]) {
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] += from[(i * FN + j) * (NW * 64) + threadIdx.x];
-    to_lds<T, NWP, NWQ>(acc, out);
-    __syncthreads();
-    finish<STAGE, T, NW * 64>(a, st, s, out);
+            for (int j = 0; j < FN; ++j) acc[i][j] = mfma_half(acc[i][j], p[i], q[j]);
+    };
+    // A step's fragments: its halves, or its high and low parts.
+    struct Fragments {
+        uint4 p[2][FM], q[2][FN];
+    };
+    auto read = [&](Fragments& f, int step) {
+        const char* at = lds + step % RING * STEP;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            OQ::fragments(at + TILE, frag_q, h, f.q[h]);
+            OP::fragments(at, frag_p, h, f.p[h]);
+        }
+    };
+    auto product = [&](const Fragments& f) {
+        multiply(f.p[0], f.q[0]);
+        multiply(f.p[PAIR ? 0 : 1], f.q[1]);
+        if (PAIR) multiply(f.p[1], f.q[0]);
+        // one or two reads between every few matrix instructions
+        constexpr int READS = 2 * (FM * (STAGE == UPDATE ? 2 : 1) + FN), MUL = FM * FN * (PAIR ? 3 : 2);
+#pragma unroll
+        for (int i = 0; i < READS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                    // an LDS read
+            __builtin_amdgcn_sched_group_barrier(0x008, MUL / READS, 0);          // matrix instructions
+        }
+    };
+    // from one barrier to the next: the following steps' copies have landed
+    // everywhere, and the places of those from `k` on are free
+    auto turn = [&](int k) {
+        wait_copies<0>();
+        wait_reads();
+        barrier();
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+            if (k + RING + u < steps) copy(k + RING + u);
+    };
+
+#pragma unroll
+    for (int k = 0; k < RING; ++k)
+        if (k < steps) copy(k);
+    if (RING <= steps) wait_copies<SUB * COPIES>();
+    else wait_copies<0>();
+    barrier();
+    // While a step's matrix instructions run, the next one's fragments are read.
+    Fragments f[2];
+    read(f[0], 0);
+    for (int k0 = 0; k0 < steps; k0 += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int k = k0 + u;
+            if (u > 0 && k >= steps) break;
+            if (SUB == 1 || u > 0) turn(k + 1 - SUB);
+            read(f[u ^ 1], k + 1);   // (after the last step: what was there, unused)
+            product(f[u]);
+        }
+    }
+
+    if (st.split > 1) {
+        // as the registers lie, a wave's together
+        floatx4* mine = reinterpret_cast<floatx4*>(a.sums) + (int64_t)me * (T * T / 4) + wave * (FM * FN * 64) + (my_thread() & 63);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) mine[(i * FN + j) * 64] = acc[i][j];
+    } else {
+        pieces<STAGE, T, NWP, NWQ>(a, st, s, STAGE != UPDATE && s.i0 != s.j0, acc, reinterpret_cast<float*>(lds));
+    }
 }
 
-template <int STAGE, bool PAIR, int T, int NWP, int NWQ>
-hipError_t launch_product(const OrthoArgs& a, StepArgs st, hipStream_t s)
+// The parts of split tiles, added in order, and what becomes of them: 64 x 64
+// values a workgroup, a wave's or the whole tile's.
+template <int STAGE, int T>
+__global__ __launch_bounds__(256) void ortho_sum_kernel(OrthoArgs a, StepArgs st)
 {
-    const int rows = a.np / T, tiles = a.batch * (STAGE == UPDATE ? rows * (a.mp / T) : rows * (rows + 1) / 2);
-    st.split = STAGE == GRAM ? a.split_gram : STAGE == SQUARE ? a.split_square : a.split_update;
-    ortho_product_kernel<STAGE, PAIR, T, NWP, NWQ><<<tiles * st.split, NWP * NWQ * 64, 0, s>>>(a, st);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || st.split == 1) return e;
-    ortho_sum_kernel<STAGE, T, NWP, NWQ><<<tiles, NWP * NWQ * 64, 0, s>>>(a, st);
+    static_assert(T == 64 || T == 128, "2 x 2 waves");
+    constexpr int PER = (T / 64) * (T / 64);
+    __shared__ __align__(1024) float lds[64 * 64];
+    const Tiles tiles = tiles_of<STAGE, T>(a);
+    const int tile = blockIdx.x / PER, part = blockIdx.x % PER;
+    if (tile >= tiles.count) return;
+    Spot s = spot_of<STAGE, T>(a, tiles, tile);
+    if (!tiles.listed && a.nothing[s.mat] != 0) return;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wp = wave >> 1, wq = wave & 1;
+    // fragment (i, j) of this wave's 32 x 32
+    auto at = [&](int i, int j) { return T == 64 ? wave * 256 + (i * 2 + j) * 64 + lane : part * 1024 + ((2 * wp + i) * 4 + 2 * wq + j) * 64 + lane; };
+    const floatx4* sums = reinterpret_cast<const floatx4*>(a.sums) + (int64_t)tile * st.split * (T * T / 4);
+    floatx4 acc[2][2] = {};
+    constexpr int AHEAD = 4;   // parts whose loads are in flight
+    for (int z = 0; z < st.split; z += AHEAD) {
+        floatx4 v[AHEAD][2][2];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) v[k][i][j] = sums[(int64_t)min(z + k, st.split - 1) * (T * T / 4) + at(i, j)];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (z + k < st.split)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[i][j] += v[k][i][j];
+    }
+    const bool mirror = STAGE != UPDATE && s.i0 != s.j0;
+    if (T == 128) {
+        s.j0 += part / 2 * 64;
+        s.i0 += part % 2 * 64;
+    }
+    pieces<STAGE, 64, 2, 2>(a, st, s, mirror, acc, lds);
+}
+
+template <int STAGE, bool PAIR, int T, int NWP, int NWQ, int SUB>
+hipError_t launch_tiles(const OrthoArgs& a, StepArgs st, const OrthoDeal& d, hipStream_t s)
+{
+    st.split = d.split;
+    ortho_product_kernel<STAGE, PAIR, T, NWP, NWQ, SUB><<<d.tiles * d.split, NWP * NWQ * 64, 0, s>>>(a, st);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || d.split == 1) return e;
+    if constexpr (NWP == 2 && NWQ == 2) ortho_sum_kernel<STAGE, T><<<d.tiles * (T / 64) * (T / 64), 256, 0, s>>>(a, st);
     return hipGetLastError();
 }
 
-template <bool PAIR, int T, int NWP, int NWQ>
-hipError_t launch_step(const OrthoArgs& a, const StepArgs& st, hipStream_t s)
+template <int STAGE, bool PAIR>
+hipError_t launch_product(const OrthoArgs& a, const StepArgs& st, const OrthoDeal& d, hipStream_t s)
 {
-    hipError_t e = launch_product<GRAM, PAIR, T, NWP, NWQ>(a, st, s);
-    if (e == hipSuccess) e = launch_product<SQUARE, PAIR, T, NWP, NWQ>(a, st, s);
-    if (e == hipSuccess) e = launch_product<UPDATE, PAIR, T, NWP, NWQ>(a, st, s);
+    switch (d.side) {
+    case 128:
+        if (d.tiles > CBW_NUM_CUS) return launch_tiles<STAGE, PAIR, 128, 2, 2, 1>(a, st, d, s);
+        if (d.split == 1) return launch_tiles<STAGE, PAIR, 128, 2, 4, 2>(a, st, d, s);
+        return launch_tiles<STAGE, PAIR, 128, 2, 2, 2>(a, st, d, s);
+    default: return launch_tiles<STAGE, PAIR, 64, 2, 2, 2>(a, st, d, s);
+    }
+}
+
+template <bool PAIR>
+hipError_t launch_step(const OrthoArgs& a, const StepArgs& st, const OrthoPlan& p, hipStream_t s)
+{
+    const OrthoDeal* d = p.deal[PAIR];
+    hipError_t e = launch_product<GRAM, PAIR>(a, st, d[GRAM], s);
+    if (e == hipSuccess) e = launch_product<SQUARE, PAIR>(a, st, d[SQUARE], s);
+    if (e == hipSuccess) e = launch_product<UPDATE, PAIR>(a, st, d[UPDATE], s);
     return e;
 }
 
 int64_t round_up(int64_t v, int64_t by) { return (v + by - 1) / by * by; }
 size_t region(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+
+// How a product of `tiles(side)` tiles of `len` reduction indices is dealt out.
+template <typename F>
+OrthoDeal deal(F tiles, int64_t len, bool pair, bool by128)
+{
+    OrthoDeal d{};
+    // (tiles past 64 are finished by pieces of 128: both sides are filled up to that)
+    d.side = !by128 ? 64 : tiles(128) >= 64 ? 128 : 64;
+    d.tiles = (int)tiles(d.side);
+    const int64_t steps = len / (pair ? 32 : 64);
+    d.split = d.side == 256 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(CBW_NUM_CUS / std::max(d.tiles, 1), steps / 4));
+    return d;
+}
 
 }  // namespace
 
@@ -491,44 +718,46 @@ OrthoPlan ortho_plan(const cbw_ortho_desc* d)
 {
     OrthoPlan p{};
     const int64_t n = std::min(d->rows, d->cols), m = std::max(d->rows, d->cols);
-    p.tile = n > 256 ? 128 : 64;
-    p.np = (int)round_up(n, p.tile);
-    p.mp = (int)round_up(m, p.tile);
-    const int64_t elements = (int64_t)d->rows * d->cols;
-    p.parts = (int)std::min<int64_t>(256, std::max<int64_t>(1, elements / 8192));
-    const int64_t rows = p.np / p.tile, tri = d->batch * rows * (rows + 1) / 2, full = d->batch * rows * (p.mp / p.tile);
-    auto split = [&](int64_t tiles, int64_t len) {
-        return (int)std::max<int64_t>(1, std::min<int64_t>(CBW_NUM_CUS / std::max<int64_t>(tiles, 1), len / 64 / 2));
-    };
-    p.split_gram = split(tri, p.mp);
-    p.split_square = split(tri, p.np);
-    p.split_update = split(full, p.np);
-    p.tiles = std::max(std::max(tri * p.split_gram, tri * p.split_square), full * p.split_update);
+    p.np = (int)round_up(n, n > 256 ? 128 : 64);
+    p.mp = (int)round_up(m, n > 256 ? 128 : 64);
+    // steps on high parts: see above (n itself, not what it is filled up to)
+    if (d->out_dtype == CBW_BF16)
+        for (double g = 1.0; p.coarse + 2 < d->steps && g <= 0.14 * (double)n; g *= (double)d->a * d->a) ++p.coarse;
+    p.parts = (int)std::min<int64_t>(512, std::max<int64_t>(1, (int64_t)d->rows * d->cols / 8192));
+    size_t sums = 0;
+    for (int pair = 0; pair < 2; ++pair) {
+        for (int k = 0; k < 3; ++k) {
+            auto tiles = [&](int side) {
+                const int64_t rows = (p.np + side - 1) / side, cols = (p.mp + side - 1) / side;
+                return d->batch * (k == UPDATE ? rows * cols : rows * (rows + 1) / 2);
+            };
+            OrthoDeal& e = p.deal[pair][k];
+            e = deal(tiles, k == GRAM ? p.mp : p.np, pair, p.np % 128 == 0 && p.mp % 128 == 0);
+            if (e.split > 1) sums = std::max(sums, (size_t)e.tiles * e.split * e.side * e.side * 4);
+        }
+    }
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
         at += region(bytes);
         return here;
     };
-    const size_t x = (size_t)d->batch * p.np * p.mp, g = (size_t)d->batch * p.np * p.np, t = (size_t)p.tile * p.tile * 4;
+    const size_t x = (size_t)d->batch * p.np * p.mp, g = (size_t)d->batch * p.np * p.np;
     p.partial = take((size_t)d->batch * p.parts * sizeof(double));
+    p.nothing = take((size_t)d->batch * 4);
     p.x = take(x * 4);
     p.planes[0] = take(x * 4);
     p.planes[1] = take(x * 4);
     p.gram = take(g * 4);
     p.poly = take(g * 4);
-    size_t sums = 0;
-    if (p.split_gram > 1) sums = std::max(sums, (size_t)tri * p.split_gram * t);
-    if (p.split_square > 1) sums = std::max(sums, (size_t)tri * p.split_square * t);
-    if (p.split_update > 1) sums = std::max(sums, (size_t)full * p.split_update * t);
     p.sums = take(sums);
     p.ws_bytes = at;
     return p;
 }
 
-hipError_t launch_orthogonalize(const OrthoArgs& a, int tile, int steps, hipStream_t s)
+hipError_t launch_orthogonalize(const OrthoArgs& a, const OrthoPlan& p, int steps, hipStream_t s)
 {
-    auto pair = [&](int k) { return a.out_f32 || k + 2 >= steps; };
+    auto pair = [&](int k) { return k >= p.coarse; };
     ortho_norm_kernel<<<a.batch * a.parts, 256, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -540,8 +769,7 @@ hipError_t launch_orthogonalize(const OrthoArgs& a, int tile, int steps, hipStre
         st.last = k + 1 == steps;
         st.pair = pair(k);
         st.next_pair = pair(k + 1);
-        if (tile == 128) e = st.pair ? launch_step<true, 128, 2, 4>(a, st, s) : launch_step<false, 128, 2, 4>(a, st, s);
-        else e = st.pair ? launch_step<true, 64, 2, 2>(a, st, s) : launch_step<false, 64, 2, 2>(a, st, s);
+        e = st.pair ? launch_step<true>(a, st, p, s) : launch_step<false>(a, st, p, s);
     }
     return e;
 }
