@@ -175,9 +175,19 @@ struct OrthoPlan {
     int coarse;                             // steps on high parts alone, the first ones
     int parts;                              // partial sums of a matrix's norm
     OrthoDeal deal[2][3];                   // on high parts and on pairs: of A, A A and B X
+    int rows, width, panels;                // up to 64 rows: X in panels of columns; rows 0: as above
     size_t partial, nothing, x, planes[2], gram, poly, sums, ws_bytes;   // byte offsets
 };
 OrthoPlan ortho_plan(const cbw_ortho_desc* d);
+// The next region of the workspace: where it begins; `at` moves on.
+inline size_t ortho_region(size_t& at, size_t bytes)
+{
+    const size_t here = at;
+    at += (bytes + 255) & ~(size_t)255;
+    return here;
+}
+// Whether the matrices are of the kind that goes by panels, and then its plan.
+bool ortho_narrow_plan(const cbw_ortho_desc* d, OrthoPlan* p);
 
 struct OrthoArgs {
     const void* m;
@@ -200,6 +210,12 @@ struct StepArgs {
     int split;                  // workgroups that share a tile's reduction
     bool last, pair, next_pair;
 };
+struct PanelArgs {
+    int width, panels, from;    // which of the two sets of A's parts is read
+    bool last;
+};
+hipError_t launch_ortho_norm(const OrthoArgs& a, hipStream_t s);
+hipError_t launch_ortho_narrow(const OrthoArgs& a, const OrthoPlan& p, int steps, hipStream_t s);
 hipError_t launch_orthogonalize(const OrthoArgs& a, const OrthoPlan& p, int steps, hipStream_t s);
 
 }  // namespace cbw

@@ -23,6 +23,7 @@
 #include "common.hpp"
 #include "block_kernels.hpp"
 #include "expert_tiles.hpp"
+#include "ortho_io.hpp"
 #include "tiles.hpp"
 
 #include <algorithm>
@@ -76,25 +77,6 @@ __device__ __forceinline__ void join(const Pair& p, float (&v)[8])
 
 // ------------------------------------------------------- norm and first X
 
-__device__ __forceinline__ float load_value(const void* p, int64_t i, bool f32)
-{
-    return f32 ? static_cast<const float*>(p)[i] : __uint_as_float((uint32_t) static_cast<const uint16_t*>(p)[i] << 16);
-}
-// Eight values from p's element i on, 16-byte aligned.
-__device__ __forceinline__ void load_values(const void* p, int64_t i, bool f32, float (&v)[8])
-{
-    if (f32) {
-        const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
-        const float4 y = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i + 4);
-        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
-    } else {
-        const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
-        const uint32_t b[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(k & 1 ? b[k / 2] & 0xffff0000u : b[k / 2] << 16);
-    }
-}
-
 // Sums of squares of a matrix, in 64 bits: part z of a.parts takes every
 // a.parts-th chunk.  Contiguous matrices are one long row.
 constexpr int kChunk = 8192;
@@ -138,18 +120,6 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(OrthoArgs a)
     if (threadIdx.x == 0) a.partial[(int64_t)mat * a.parts + z] = sums[0] + sums[1] + sums[2] + sums[3];
 }
 
-// 1 / (|M| + eps).  A norm that is no number, or infinite, leaves no number
-// anywhere; nothing stays nothing.  Called by whole waves.
-__device__ __forceinline__ double inverse_norm(const OrthoArgs& a, int mat, bool& nothing)
-{
-    double s = 0.0;
-    for (int z = threadIdx.x & 63; z < a.parts; z += 64) s += a.partial[(int64_t)mat * a.parts + z];
-    for (int k = 32; k >= 1; k >>= 1) s += __shfl_xor(s, k);
-    const double norm = sqrt(s), all = norm + a.eps;
-    nothing = norm == 0.0;
-    return all > 0.0 ? (norm < __builtin_inf() ? 1.0 / all : __builtin_nan("")) : all == 0.0 ? 0.0 : all;
-}
-
 // Where a matrix's planes of `ld` columns and `rows` rows (of one matrix) hold
 // the high part of (i, j), and how much further its low part lies.  Products
 // on pairs find 32 high parts and the same columns' 32 low parts in each 128
@@ -174,36 +144,6 @@ __device__ __forceinline__ void put_x(const OrthoArgs& a, const Plane& plane, _F
     const Pair w = split(v);
     *reinterpret_cast<uint4*>(to + plane.at(i, j)) = w.hi;
     if (plane.pair) *reinterpret_cast<uint4*>(to + plane.at(i, j) + plane.low) = w.lo;
-}
-
-// Eight values of a row of the output, from column `col` on.
-__device__ __forceinline__ void store_out(const OrthoArgs& a, int mat, int row, int col, const float (&v)[8])
-{
-    if (row >= a.rows || col >= a.cols) return;
-    const int64_t at = ((int64_t)mat * a.rows + row) * a.out_stride + col;
-    const int n = min(8, a.cols - col);
-    if (a.out_f32) {
-        float* o = static_cast<float*>(a.o) + at;
-        if (n == 8 && ((uintptr_t)o & 15) == 0) {
-            *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<float4*>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (k < n) o[k] = v[k];
-        }
-    } else {
-        uint16_t* o = static_cast<uint16_t*>(a.o) + at;
-        const uint4 w = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-        if (n == 8 && ((uintptr_t)o & 15) == 0) {
-            *reinterpret_cast<uint4*>(o) = w;
-        } else {
-            const uint32_t b[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (k < n) o[k] = (uint16_t)(b[k / 2] >> 16 * (k & 1));
-        }
-    }
 }
 
 // X and its planes, 64 x 64 values a workgroup, zeros past the matrix.
@@ -697,7 +637,6 @@ hipError_t launch_step(const OrthoArgs& a, const StepArgs& st, const OrthoPlan& 
 }
 
 int64_t round_up(int64_t v, int64_t by) { return (v + by - 1) / by * by; }
-size_t region(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
 // How a product of `tiles(side)` tiles of `len` reduction indices is dealt out.
 template <typename F>
@@ -718,6 +657,7 @@ OrthoPlan ortho_plan(const cbw_ortho_desc* d)
 {
     OrthoPlan p{};
     const int64_t n = std::min(d->rows, d->cols), m = std::max(d->rows, d->cols);
+    if (ortho_narrow_plan(d, &p)) return p;
     p.np = (int)round_up(n, n > 256 ? 128 : 64);
     p.mp = (int)round_up(m, n > 256 ? 128 : 64);
     // steps on high parts: see above (n itself, not what it is filled up to)
@@ -737,11 +677,7 @@ OrthoPlan ortho_plan(const cbw_ortho_desc* d)
         }
     }
     size_t at = 0;
-    auto take = [&](size_t bytes) {
-        const size_t here = at;
-        at += region(bytes);
-        return here;
-    };
+    auto take = [&](size_t bytes) { return ortho_region(at, bytes); };
     const size_t x = (size_t)d->batch * p.np * p.mp, g = (size_t)d->batch * p.np * p.np;
     p.partial = take((size_t)d->batch * p.parts * sizeof(double));
     p.nothing = take((size_t)d->batch * 4);
@@ -755,11 +691,17 @@ OrthoPlan ortho_plan(const cbw_ortho_desc* d)
     return p;
 }
 
+hipError_t launch_ortho_norm(const OrthoArgs& a, hipStream_t s)
+{
+    ortho_norm_kernel<<<a.batch * a.parts, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
 hipError_t launch_orthogonalize(const OrthoArgs& a, const OrthoPlan& p, int steps, hipStream_t s)
 {
+    if (p.rows) return launch_ortho_narrow(a, p, steps, s);
     auto pair = [&](int k) { return k >= p.coarse; };
-    ortho_norm_kernel<<<a.batch * a.parts, 256, 0, s>>>(a);
-    hipError_t e = hipGetLastError();
+    hipError_t e = launch_ortho_norm(a, s);
     if (e != hipSuccess) return e;
     ortho_start_kernel<<<a.batch * (a.np / 64) * (a.mp / 64), 256, 0, s>>>(a, pair(0));
     if ((e = hipGetLastError()) != hipSuccess) return e;

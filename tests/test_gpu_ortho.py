@@ -39,7 +39,9 @@ def _run(m, out="f32", dtype="f32", coefficients=QUINTIC, steps=5, eps=1e-7):
 
 
 SIZES = [(1, 1, 1), (2, 1, 7), (2, 7, 1), (3, 5, 3), (2, 3, 40), (1, 1, 5000), (1, 4100, 2), (2, 64, 64), (1, 63, 65), (1, 64, 576),
-         (2, 200, 104), (1, 129, 300), (3, 300, 129), (1, 257, 260), (2, 333, 257), (1, 513, 100), (1, 100, 2000), (1, 384, 640), (1, 300, 1500)]
+         (2, 200, 104), (1, 129, 300), (3, 300, 129), (1, 257, 260), (2, 333, 257), (1, 513, 100), (1, 100, 2000), (1, 384, 640), (1, 300, 1500),
+         (2, 16, 2048), (1, 2049, 16), (1, 13, 50000), (2, 17, 500), (1, 600, 32), (1, 20, 9000), (2, 33, 128), (1, 64, 129), (1, 50, 6100),
+         (1, 40, 6200), (70, 9, 30), (3, 65, 64)]
 
 
 @pytest.mark.parametrize("out", ["f32", "bf16"])

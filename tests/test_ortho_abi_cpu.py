@@ -71,17 +71,18 @@ def test_coefficients(L, coefficients, steps):
 def test_workspace(L):
     n = cb.cbw_ortho_workspace_size(_desc(rows=1024, cols=2048, batch=3))
     assert 3 * 1024 * 2048 * 12 <= n <= 3 * 1024 * 2048 * 12 + 3 * 1024 * 1024 * 8 + (1 << 26)
-    assert cb.cbw_ortho_workspace_size(_desc(batch=0)) == 0
+    assert cb.cbw_ortho_workspace_size(_desc(batch=0)) == cb.cbw_ortho_workspace_size(_desc()) == 0    # (one panel: all in the LDS)
     with pytest.raises(cb.CbwError):
         cb.cbw_ortho_workspace_size(_desc(rows=0))
     assert L.cbw_ortho_workspace_size(ctypes.byref(_desc()), None) == INV
 
 
 def test_refusals(L):
-    n = cb.cbw_ortho_workspace_size(_desc())
+    n = cb.cbw_ortho_workspace_size(_desc(rows=300, cols=200))
+    assert n > 0
 
     def call(d=None, M=FAKE, O=ODD, ws=FAKE, nb=n):
-        return L.grad_orthogonalize(ctypes.byref(d or _desc()), M, O, ws, nb, None)
+        return L.grad_orthogonalize(ctypes.byref(d or _desc(rows=300, cols=200)), M, O, ws, nb, None)
 
     assert call(M=None) == call(O=None) == call(d=_desc(rows=0)) == INV
     assert call(O=FAKE, d=_desc(out_dtype="bf16")) == call(O=FAKE, d=_desc(out_stride=70)) == INV     # in place, not alike
