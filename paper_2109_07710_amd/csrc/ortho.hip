@@ -560,22 +560,20 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs 
     }
 }
 
-// The parts of split tiles, added in order, and what becomes of them: 64 x 64
-// values a workgroup, a wave's or the whole tile's.
-template <int STAGE, int T>
+// The parts of split tiles of 64 x 64, added in order, and what becomes of them.
+template <int STAGE>
 __global__ __launch_bounds__(256) void ortho_sum_kernel(OrthoArgs a, StepArgs st)
 {
-    static_assert(T == 64 || T == 128, "2 x 2 waves");
-    constexpr int PER = (T / 64) * (T / 64);
-    __shared__ __align__(1024) float lds[64 * 64];
+    constexpr int T = 64;
+    __shared__ __align__(1024) float lds[T * T];
     const Tiles tiles = tiles_of<STAGE, T>(a);
-    const int tile = blockIdx.x / PER, part = blockIdx.x % PER;
+    const int tile = blockIdx.x;
     if (tile >= tiles.count) return;
-    Spot s = spot_of<STAGE, T>(a, tiles, tile);
+    const Spot s = spot_of<STAGE, T>(a, tiles, tile);
     if (!tiles.listed && a.nothing[s.mat] != 0) return;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wp = wave >> 1, wq = wave & 1;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     // fragment (i, j) of this wave's 32 x 32
-    auto at = [&](int i, int j) { return T == 64 ? wave * 256 + (i * 2 + j) * 64 + lane : part * 1024 + ((2 * wp + i) * 4 + 2 * wq + j) * 64 + lane; };
+    auto at = [&](int i, int j) { return wave * 256 + (i * 2 + j) * 64 + lane; };
     const floatx4* sums = reinterpret_cast<const floatx4*>(a.sums) + (int64_t)tile * st.split * (T * T / 4);
     floatx4 acc[2][2] = {};
     constexpr int AHEAD = 4;   // parts whose loads are in flight
@@ -595,12 +593,7 @@ __global__ __launch_bounds__(256) void ortho_sum_kernel(OrthoArgs a, StepArgs st
 #pragma unroll
                     for (int j = 0; j < 2; ++j) acc[i][j] += v[k][i][j];
     }
-    const bool mirror = STAGE != UPDATE && s.i0 != s.j0;
-    if (T == 128) {
-        s.j0 += part / 2 * 64;
-        s.i0 += part % 2 * 64;
-    }
-    pieces<STAGE, 64, 2, 2>(a, st, s, mirror, acc, lds);
+    pieces<STAGE, T, 2, 2>(a, st, s, STAGE != UPDATE && s.i0 != s.j0, acc, lds);
 }
 
 template <int STAGE, bool PAIR, int T, int NWP, int NWQ, int SUB>
@@ -610,7 +603,7 @@ hipError_t launch_tiles(const OrthoArgs& a, StepArgs st, const OrthoDeal& d, hip
     ortho_product_kernel<STAGE, PAIR, T, NWP, NWQ, SUB><<<d.tiles * d.split, NWP * NWQ * 64, 0, s>>>(a, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || d.split == 1) return e;
-    if constexpr (NWP == 2 && NWQ == 2) ortho_sum_kernel<STAGE, T><<<d.tiles * (T / 64) * (T / 64), 256, 0, s>>>(a, st);
+    if constexpr (T == 64) ortho_sum_kernel<STAGE><<<d.tiles, 256, 0, s>>>(a, st);
     return hipGetLastError();
 }
 
@@ -619,10 +612,14 @@ hipError_t launch_product(const OrthoArgs& a, const StepArgs& st, const OrthoDea
 {
     switch (d.side) {
     case 128:
+        // two workgroups to a CU where there are as many, else twice the steps to a
+        // barrier and twice the waves (2048 x 2048, A | A A | B X, us: 25 | 25 | 31 for
+        // 27 | 28 | 33 with four waves, and 28 | 29 | 34 with half the steps)
         if (d.tiles > CBW_NUM_CUS) return launch_tiles<STAGE, PAIR, 128, 2, 2, 1>(a, st, d, s);
-        if (d.split == 1) return launch_tiles<STAGE, PAIR, 128, 2, 4, 2>(a, st, d, s);
-        return launch_tiles<STAGE, PAIR, 128, 2, 2, 2>(a, st, d, s);
-    default: return launch_tiles<STAGE, PAIR, 64, 2, 2, 2>(a, st, d, s);
+        return launch_tiles<STAGE, PAIR, 128, 2, 4, 2>(a, st, d, s);
+    default:
+        if (d.tiles * d.split > CBW_NUM_CUS) return launch_tiles<STAGE, PAIR, 64, 2, 2, 1>(a, st, d, s);
+        return launch_tiles<STAGE, PAIR, 64, 2, 2, 2>(a, st, d, s);
     }
 }
 
@@ -639,15 +636,26 @@ hipError_t launch_step(const OrthoArgs& a, const StepArgs& st, const OrthoPlan& 
 int64_t round_up(int64_t v, int64_t by) { return (v + by - 1) / by * by; }
 
 // How a product of `tiles(side)` tiles of `len` reduction indices is dealt out.
+// Tiles of 64 take some 0.5 us a step beside 4.4 for the start and the end; the
+// parts of a split one 2 beside their steps, and the launch that adds them up
+// 3.5 and 0.25 a part (us, 3 x 333 x 1001 and 256 x 2304, measured by launches).
 template <typename F>
 OrthoDeal deal(F tiles, int64_t len, bool pair, bool by128)
 {
     OrthoDeal d{};
-    // (tiles past 64 are finished by pieces of 128: both sides are filled up to that)
-    d.side = !by128 ? 64 : tiles(128) >= 64 ? 128 : 64;
+    // (those of 128 are finished whole: both sides are filled up to that)
+    d.side = by128 && tiles(128) >= 128 ? 128 : 64;
     d.tiles = (int)tiles(d.side);
+    d.split = 1;
     const int64_t steps = len / (pair ? 32 : 64);
-    d.split = d.side == 256 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(CBW_NUM_CUS / std::max(d.tiles, 1), steps / 4));
+    double best = 4.4 + 0.5 * (double)steps - 1.0;   // (no split for less than 1 us)
+    for (int s = 2; d.side == 64 && s <= steps && s <= 24 && (int64_t)d.tiles * s <= 2 * CBW_NUM_CUS; ++s) {
+        const double us = 5.5 + 0.25 * s + 0.5 * (double)((steps + s - 1) / s);
+        if (us < best) {
+            best = us;
+            d.split = s;
+        }
+    }
     return d;
 }
 

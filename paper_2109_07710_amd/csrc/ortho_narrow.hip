@@ -18,20 +18,29 @@
 #include "tiles.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace cbw {
 namespace {
 
-// NB blocks of 16 rows, panels of up to W columns.  Rows lie four values more
+constexpr int kWaves = 8, kThreads = kWaves * 64;
+
+// NB blocks of 16 rows, panels of up to W columns.  The waves stand side by side
+// over COLS blocks of 16 columns; with four blocks of rows, two waves share a
+// block of columns and take half of what is to be computed each.  Rows lie four values more
 // than their length apart, so that neither 16 rows' vectors nor a column's
 // values share banks.
 template <int NB, int W>
 struct Narrow {
     static constexpr int NP = 16 * NB, LD = W + 4, LDA = NP + 4, TRI = NB * (NB + 1) / 2;
+    static constexpr int SHARE = NB == 4 ? 2 : 1, COLS = kWaves / SHARE;
     float x[NP * LD];
-    float a[NP * LDA], b[NP * LDA];
-    floatx4 parts[4][TRI][64];   // the waves' parts of A's blocks on and below the diagonal
-    double sums[4];
+    float a[NP * LDA];
+    union {
+        float b[NP * LDA];
+        floatx4 parts[COLS][TRI][64];   // the waves' parts of A's blocks on and below the diagonal, while there is no B
+        double sums[kWaves];            // of the norm, before either
+    };
 };
 
 // block row and column of the t-th block on or below the diagonal
@@ -60,16 +69,32 @@ template <int NB, int W>
 __device__ __forceinline__ void panel_gram(Narrow<NB, W>& l, int width)
 {
     using N = Narrow<NB, W>;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    floatx4 acc[N::TRI] = {};
-    for (int c = wave * 16; c < width; c += 64) {
-        floatx4 f[NB];
+    constexpr int MINE = N::TRI / N::SHARE;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = wave % N::COLS, t0 = wave / N::COLS * MINE;
+    floatx4 acc[MINE] = {};
+    // (the blocks' numbers are known to the compiler: the two halves are two loops)
+    auto run = [&](auto half) {
+        for (int c = col * 16; c < width; c += N::COLS * 16) {
+            floatx4 f[NB];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) f[b] = vector_at(l.x + (b * 16 + (lane & 15)) * N::LD + c + 4 * (lane >> 4));
-        multiply(acc, [&](int t) { return f[row_block(t)]; }, [&](int t) { return f[t - row_block(t) * (row_block(t) + 1) / 2]; });
-    }
+            for (int b = 0; b < NB; ++b) f[b] = vector_at(l.x + (b * 16 + (lane & 15)) * N::LD + c + 4 * (lane >> 4));
+            auto row = [&](int t) { return row_block(t + half.value * MINE); };
+            multiply(acc, [&](int t) { return f[row(t)]; }, [&](int t) { return f[t + half.value * MINE - row(t) * (row(t) + 1) / 2]; });
+        }
+    };
+    if (N::SHARE == 1 || t0 == 0) run(std::integral_constant<int, 0>());
+    else run(std::integral_constant<int, N::SHARE - 1>());
 #pragma unroll
-    for (int t = 0; t < N::TRI; ++t) l.parts[wave][t][lane] = acc[t];
+    for (int t = 0; t < MINE; ++t) l.parts[col][t0 + t][lane] = acc[t];
+}
+// The sum of the waves' parts of A's t-th vector.
+template <int NB, int W>
+__device__ __forceinline__ floatx4 sum_of_parts(const Narrow<NB, W>& l, int t)
+{
+    floatx4 s = l.parts[0][t / 64][t % 64];
+#pragma unroll
+    for (int k = 1; k < Narrow<NB, W>::COLS; ++k) s += l.parts[k][t / 64][t % 64];
+    return s;
 }
 
 // Four rows r .. r + 3 of column c of a symmetric matrix's block (bi, bj), into both places.
@@ -88,12 +113,12 @@ __device__ __forceinline__ void polynomial(Narrow<NB, W>& l, float cb, float cc)
 {
     using N = Narrow<NB, W>;
     const int lane = threadIdx.x & 63;
-    // a wave's blocks, wave, wave + 4, ... (a last one too many is the last block again)
-    constexpr int MINE = (N::TRI + 3) / 4;
+    // a wave's blocks, wave, wave + 8 (one too many is the last block again)
+    constexpr int MINE = (N::TRI + kWaves - 1) / kWaves;
     const int wave = threadIdx.x >> 6, r = lane & 15, k4 = 4 * (lane >> 4);
     int bi[MINE], bj[MINE];
 #pragma unroll
-    for (int i = 0; i < MINE; ++i) block_of(min(wave + 4 * i, N::TRI - 1), bi[i], bj[i]);
+    for (int i = 0; i < MINE; ++i) block_of(min(wave + kWaves * i, N::TRI - 1), bi[i], bj[i]);
     floatx4 s[MINE] = {};
 #pragma unroll
     for (int k = 0; k < NB; ++k)
@@ -101,7 +126,7 @@ __device__ __forceinline__ void polynomial(Narrow<NB, W>& l, float cb, float cc)
                  [&](int i) { return vector_at(l.a + (bj[i] * 16 + r) * N::LDA + k * 16 + k4); });
 #pragma unroll
     for (int i = 0; i < MINE; ++i) {
-        if (wave + 4 * i >= N::TRI) break;
+        if (wave + kWaves * i >= N::TRI) break;
 #pragma unroll
         for (int k = 0; k < 4; ++k) s[i][k] = cb * l.a[(bi[i] * 16 + k4 + k) * N::LDA + bj[i] * 16 + r] + cc * s[i][k];
         put_block<N::LDA>(l.b, bi[i], bj[i], lane, s[i]);
@@ -114,49 +139,71 @@ template <int NB, int W>
 __device__ __forceinline__ void panel_update(Narrow<NB, W>& l, int width, float ca)
 {
     using N = Narrow<NB, W>;
-    const int lane = threadIdx.x & 63;
-    for (int c = (threadIdx.x >> 6) * 16; c < width; c += 64) {
+    constexpr int MINE = NB / N::SHARE;   // blocks of rows of the result
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = wave % N::COLS, b0 = wave / N::COLS * MINE;
+    for (int c0 = 0; c0 < width; c0 += N::COLS * 16) {
+        const int c = c0 + col * 16;
         float* at = l.x + 4 * (lane >> 4) * N::LD + c + (lane & 15);
-        floatx4 x[NB];
+        floatx4 x[NB], s[MINE] = {};
+        if (c < width) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[b][k] = at[(b * 16 + k) * N::LD];
-        floatx4 s[NB] = {};
+                for (int k = 0; k < 4; ++k) x[b][k] = at[(b * 16 + k) * N::LD];
 #pragma unroll
-        for (int k = 0; k < NB; ++k)
-            multiply(s, [&](int i) { return vector_at(l.b + (i * 16 + (lane & 15)) * N::LDA + k * 16 + 4 * (lane >> 4)); },
-                     [&](int) { return x[k]; });
+            for (int k = 0; k < NB; ++k)
+                multiply(s, [&](int i) { return vector_at(l.b + ((b0 + i) * 16 + (lane & 15)) * N::LDA + k * 16 + 4 * (lane >> 4)); },
+                         [&](int) { return x[k]; });
+        }
+        if (N::SHARE > 1) __syncthreads();   // the other wave has read its columns as well
+        if (c < width)
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+            for (int i = 0; i < MINE; ++i)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) at[(b * 16 + k) * N::LD] = ca * x[b][k] + s[b][k];
+                for (int k = 0; k < 4; ++k) {
+                    const float old = N::SHARE == 1 || b0 == 0 ? x[i][k] : x[MINE * (N::SHARE - 1) + i][k];
+                    at[((b0 + i) * 16 + k) * N::LD] = ca * old + s[i][k];
+                }
     }
 }
 
-// The panel's values of M (columns p0 on of X), zeros past the matrix; their
-// sum of squares.
+// The panel's values of M (columns p0 on of X), zeros past the matrix; the
+// thread's share of their sum of squares.
 template <int NB, int W>
 __device__ __forceinline__ double load_panel(Narrow<NB, W>& l, const OrthoArgs& a, int mat, int p0, int width)
 {
     using N = Narrow<NB, W>;
-    const int n = a.tall ? a.cols : a.rows, m = a.tall ? a.rows : a.cols;
+    // vectors along M's rows: `across` of them to a row of the panel, or (tall) to a row of M
+    const int across = (a.tall ? N::NP : width) / 8, vectors = N::NP * width / 8;
     const int64_t base = (int64_t)mat * a.rows * a.in_stride;
+    const int size = a.in_f32 ? 4 : 2;
     double s = 0.0;
-    auto place = [&](int i, int c) {
-        float v = 0.f;
-        if (i < n && p0 + c < m) v = load_value(a.m, base + (a.tall ? (int64_t)(p0 + c) * a.in_stride + i : (int64_t)i * a.in_stride + p0 + c), a.in_f32);
-        l.x[i * N::LD + c] = v;
-        s += (double)v * v;
-    };
-    // (consecutive threads take consecutive values of a row of M)
-    if (a.tall) {
-#pragma unroll 4
-        for (int t = threadIdx.x; t < width * N::NP; t += 256) place(t % N::NP, t / N::NP);
-    } else {
-        for (int i = threadIdx.x >> 6; i < N::NP; i += 4)
-#pragma unroll 4
-            for (int c = threadIdx.x & 63; c < width; c += 64) place(i, c);
+    constexpr int AHEAD = 4;   // vectors whose loads are in flight
+    for (int t0 = threadIdx.x; t0 < vectors; t0 += AHEAD * kThreads) {
+        float v[AHEAD][8];
+#pragma unroll
+        for (int h = 0; h < AHEAD; ++h) {
+            const int t = t0 + h * kThreads, row = t / across + (a.tall ? p0 : 0), col = t % across * 8 + (a.tall ? 0 : p0);
+            const int64_t at = base + row * a.in_stride + col;
+            const bool in = t < vectors && row < a.rows;
+            if (in && col + 8 <= a.cols && ((uintptr_t)a.m + at * size) % 16 == 0) {
+                load_values(a.m, at, a.in_f32, v[h]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[h][k] = in && col + k < a.cols ? load_value(a.m, at + k, a.in_f32) : 0.f;
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < AHEAD; ++h) {
+            const int t = t0 + h * kThreads, r = t / across, c = t % across * 8;
+            if (t >= vectors) break;
+            float* to = a.tall ? l.x + c * N::LD + r : l.x + r * N::LD + c;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                to[k * (a.tall ? N::LD : 1)] = v[h][k];
+                s += (double)v[h][k] * v[h][k];
+            }
+        }
     }
     return s;
 }
@@ -168,7 +215,7 @@ __device__ __forceinline__ void scale_panel(Narrow<NB, W>& l, const OrthoArgs& a
 {
     using N = Narrow<NB, W>;
     const int n = a.tall ? a.cols : a.rows, m = a.tall ? a.rows : a.cols;
-    for (int i = threadIdx.x >> 6; i < n; i += 4)
+    for (int i = threadIdx.x >> 6; i < n; i += kWaves)
         for (int c = threadIdx.x & 63; c < min(width, m - p0); c += 64) l.x[i * N::LD + c] = (float)(l.x[i * N::LD + c] * inv);
 }
 
@@ -178,14 +225,14 @@ __device__ __forceinline__ void store_panel(const Narrow<NB, W>& l, const OrthoA
     using N = Narrow<NB, W>;
     float v[8];
     if (a.tall) {
-        for (int t = threadIdx.x; t < width * (N::NP / 8); t += 256) {
+        for (int t = threadIdx.x; t < width * (N::NP / 8); t += kThreads) {
             const int c = t / (N::NP / 8), i = t % (N::NP / 8) * 8;
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = l.x[(i + k) * N::LD + c];
             store_out(a, mat, p0 + c, i, v);
         }
     } else {
-        for (int t = threadIdx.x; t < N::NP * (width / 8); t += 256) {
+        for (int t = threadIdx.x; t < N::NP * (width / 8); t += kThreads) {
             const int i = t / (width / 8), c = t % (width / 8) * 8;
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = l.x[i * N::LD + c + k];
@@ -199,17 +246,16 @@ template <int NB, int W>
 __device__ __forceinline__ void whole_gram(Narrow<NB, W>& l)
 {
     using N = Narrow<NB, W>;
-    for (int t = threadIdx.x; t < N::TRI * 64; t += 256) {
+    for (int t = threadIdx.x; t < N::TRI * 64; t += kThreads) {
         int bi, bj;
         block_of(t / 64, bi, bj);
-        const floatx4 s = l.parts[0][t / 64][t % 64] + l.parts[1][t / 64][t % 64] + l.parts[2][t / 64][t % 64] + l.parts[3][t / 64][t % 64];
-        put_block<N::LDA>(l.a, bi, bj, t % 64, s);
+        put_block<N::LDA>(l.a, bi, bj, t % 64, sum_of_parts(l, t));
     }
 }
 
 // A matrix of one panel: a workgroup from the norm to the update.
 template <int NB, int W>
-__global__ __launch_bounds__(256) void ortho_whole_kernel(OrthoArgs a, int width, int steps)
+__global__ __launch_bounds__(kThreads) void ortho_whole_kernel(OrthoArgs a, int width, int steps)
 {
     __shared__ __align__(16) Narrow<NB, W> l;
     const int mat = blockIdx.x;
@@ -217,7 +263,9 @@ __global__ __launch_bounds__(256) void ortho_whole_kernel(OrthoArgs a, int width
     for (int k = 32; k >= 1; k >>= 1) s += __shfl_xor(s, k);
     if ((threadIdx.x & 63) == 0) l.sums[threadIdx.x >> 6] = s;
     __syncthreads();
-    scale_panel(l, a, 0, width, inverse_of(l.sums[0] + l.sums[1] + l.sums[2] + l.sums[3], a.eps));
+    s = 0.0;
+    for (int k = 0; k < kWaves; ++k) s += l.sums[k];
+    scale_panel(l, a, 0, width, inverse_of(s, a.eps));
     for (int k = 0; k < steps; ++k) {
         __syncthreads();
         panel_gram(l, width);
@@ -238,19 +286,18 @@ __device__ __forceinline__ void leave_panel(Narrow<NB, W>& l, const OrthoArgs& a
 {
     using N = Narrow<NB, W>;
     float* x = a.x + ((int64_t)mat * p.panels + panel) * N::NP * p.width;
-    for (int t = threadIdx.x; t < N::NP * (p.width / 4); t += 256) {
+    for (int t = threadIdx.x; t < N::NP * (p.width / 4); t += kThreads) {
         const int i = t / (p.width / 4), c = t % (p.width / 4) * 4;
         *reinterpret_cast<floatx4*>(x + i * p.width + c) = *reinterpret_cast<const floatx4*>(l.x + i * N::LD + c);
     }
     panel_gram(l, p.width);
     __syncthreads();
     floatx4* part = reinterpret_cast<floatx4*>(a.sums) + (((int64_t)to * a.batch + mat) * p.panels + panel) * N::TRI * 64;
-    for (int t = threadIdx.x; t < N::TRI * 64; t += 256)
-        part[t] = l.parts[0][t / 64][t % 64] + l.parts[1][t / 64][t % 64] + l.parts[2][t / 64][t % 64] + l.parts[3][t / 64][t % 64];
+    for (int t = threadIdx.x; t < N::TRI * 64; t += kThreads) part[t] = sum_of_parts(l, t);
 }
 
 template <int NB, int W>
-__global__ __launch_bounds__(256) void ortho_first_kernel(OrthoArgs a, PanelArgs p)
+__global__ __launch_bounds__(kThreads) void ortho_first_kernel(OrthoArgs a, PanelArgs p)
 {
     __shared__ __align__(16) Narrow<NB, W> l;
     const int mat = blockIdx.x / p.panels, panel = blockIdx.x - mat * p.panels;
@@ -264,19 +311,21 @@ __global__ __launch_bounds__(256) void ortho_first_kernel(OrthoArgs a, PanelArgs
 }
 
 template <int NB, int W>
-__global__ __launch_bounds__(256) void ortho_step_kernel(OrthoArgs a, PanelArgs p)
+__global__ __launch_bounds__(kThreads) void ortho_step_kernel(OrthoArgs a, PanelArgs p)
 {
     using N = Narrow<NB, W>;
     __shared__ __align__(16) N l;
     const int mat = blockIdx.x / p.panels, panel = blockIdx.x - mat * p.panels;
     const float* x = a.x + ((int64_t)mat * p.panels + panel) * N::NP * p.width;
-    for (int t = threadIdx.x; t < N::NP * (p.width / 4); t += 256) {
-        const int i = t / (p.width / 4), c = t % (p.width / 4) * 4;
-        *reinterpret_cast<floatx4*>(l.x + i * N::LD + c) = *reinterpret_cast<const floatx4*>(x + i * p.width + c);
-    }
+    const floatx4* x4 = reinterpret_cast<const floatx4*>(x);
+    constexpr int XV = 4;
+    const int vectors = N::NP * (p.width / 4);
+    floatx4 ahead[XV];   // the panel's first values, on their way while A is added up
+#pragma unroll
+    for (int h = 0; h < XV; ++h) ahead[h] = x4[min((int)threadIdx.x + h * kThreads, vectors - 1)];
     const floatx4* parts = reinterpret_cast<const floatx4*>(a.sums) + ((int64_t)p.from * a.batch + mat) * p.panels * N::TRI * 64;
     // a thread's vectors of A's blocks; eight parts' loads of all of them in flight
-    constexpr int MINE = (N::TRI * 64 + 255) / 256, AHEAD = 8;
+    constexpr int MINE = (N::TRI * 64 + kThreads - 1) / kThreads, AHEAD = 8;
     floatx4 s[MINE] = {};
     for (int z = 0; z < p.panels; z += AHEAD) {
         floatx4 v[AHEAD][MINE];
@@ -284,7 +333,7 @@ __global__ __launch_bounds__(256) void ortho_step_kernel(OrthoArgs a, PanelArgs 
         for (int k = 0; k < AHEAD; ++k)
 #pragma unroll
             for (int i = 0; i < MINE; ++i)
-                v[k][i] = parts[(int64_t)min(z + k, p.panels - 1) * N::TRI * 64 + min((int)threadIdx.x + i * 256, N::TRI * 64 - 1)];
+                v[k][i] = parts[(int64_t)min(z + k, p.panels - 1) * N::TRI * 64 + min((int)threadIdx.x + i * kThreads, N::TRI * 64 - 1)];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
             if (z + k < p.panels)
@@ -293,11 +342,21 @@ __global__ __launch_bounds__(256) void ortho_step_kernel(OrthoArgs a, PanelArgs 
     }
 #pragma unroll
     for (int i = 0; i < MINE; ++i) {
-        const int t = threadIdx.x + i * 256;
+        const int t = threadIdx.x + i * kThreads;
         if (t >= N::TRI * 64) break;
         int bi, bj;
         block_of(t / 64, bi, bj);
         put_block<N::LDA>(l.a, bi, bj, t % 64, s[i]);
+    }
+    for (int t0 = threadIdx.x; t0 < vectors; t0 += XV * kThreads) {
+        if (t0 != (int)threadIdx.x)
+#pragma unroll
+            for (int h = 0; h < XV; ++h) ahead[h] = x4[min(t0 + h * kThreads, vectors - 1)];
+#pragma unroll
+        for (int h = 0; h < XV; ++h) {
+            const int t = t0 + h * kThreads, i = t / (p.width / 4), c = t % (p.width / 4) * 4;
+            if (t < vectors) *reinterpret_cast<floatx4*>(l.x + i * N::LD + c) = ahead[h];
+        }
     }
     __syncthreads();
     polynomial(l, a.b, a.c);
@@ -312,18 +371,18 @@ template <int NB, int W>
 hipError_t launch(const OrthoArgs& a, const OrthoPlan& plan, int steps, hipStream_t s)
 {
     if (plan.panels == 1) {
-        ortho_whole_kernel<NB, W><<<a.batch, 256, 0, s>>>(a, plan.width, steps);
+        ortho_whole_kernel<NB, W><<<a.batch, kThreads, 0, s>>>(a, plan.width, steps);
         return hipGetLastError();
     }
     hipError_t e = launch_ortho_norm(a, s);
     if (e != hipSuccess) return e;
     PanelArgs p{plan.width, plan.panels, 0, false};
-    ortho_first_kernel<NB, W><<<a.batch * plan.panels, 256, 0, s>>>(a, p);
+    ortho_first_kernel<NB, W><<<a.batch * plan.panels, kThreads, 0, s>>>(a, p);
     e = hipGetLastError();
     for (int k = 0; k < steps && e == hipSuccess; ++k) {
         p.from = k & 1;
         p.last = k + 1 == steps;
-        ortho_step_kernel<NB, W><<<a.batch * plan.panels, 256, 0, s>>>(a, p);
+        ortho_step_kernel<NB, W><<<a.batch * plan.panels, kThreads, 0, s>>>(a, p);
         e = hipGetLastError();
     }
     return e;
