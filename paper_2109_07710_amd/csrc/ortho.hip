@@ -228,8 +228,9 @@ __device__ __forceinline__ Tiles tiles_of(const OrthoArgs& a)
     Tiles t;
     const int rows = (a.np + T - 1) / T, cols = (a.mp + T - 1) / T, lane = threadIdx.x & 63;
     t.per = STAGE == UPDATE ? rows * cols : rows * (rows + 1) / 2;
+    // (one matrix is looked at only before its tiles are stored: that takes no time)
     t.listed = a.batch <= 64;
-    t.busy = t.listed ? __ballot(lane < a.batch && a.nothing[lane < a.batch ? lane : 0] == 0) : 0;
+    t.busy = a.batch == 1 ? 1 : t.listed ? __ballot(lane < a.batch && a.nothing[lane < a.batch ? lane : 0] == 0) : 0;
     t.count = t.per * (t.listed ? __popcll(t.busy) : a.batch);
     return t;
 }
@@ -298,10 +299,38 @@ __device__ __forceinline__ int my_thread()
     return t;
 }
 
+// What a finished T x T piece meets: X (B X) or A (A A), the thread's vectors of
+// it, on their way while the sums are still being added up.
+template <int STAGE, int T, int THREADS>
+struct Meets {
+    static constexpr int VECS = STAGE == GRAM ? 1 : T * T / 8 / THREADS;
+    uint4 v[VECS][2];
+    __device__ __forceinline__ void load(const OrthoArgs& a, const StepArgs& st, const Spot& s)
+    {
+        if (STAGE == GRAM) return;
+        const Plane square(st.pair, s.mat, a.batch, a.np, a.np);
+        const int thread = my_thread();
+#pragma unroll
+        for (int k = 0; k < VECS; ++k) {
+            const int t = thread + k * THREADS, q = t / (T / 8), p = t % (T / 8) * 8;
+            if (STAGE == UPDATE) {
+                const uint4* x = reinterpret_cast<const uint4*>(a.x + (int64_t)s.mat * a.np * a.mp + (int64_t)(s.i0 + q) * a.mp + s.j0 + p);
+                v[k][0] = x[0];
+                v[k][1] = x[1];
+            } else {
+                const _Float16* g = a.gram + square.at(s.i0 + q, s.j0 + p);
+                v[k][0] = *reinterpret_cast<const uint4*>(g);
+                v[k][1] = *reinterpret_cast<const uint4*>(g + square.low);
+            }
+        }
+    }
+};
+
 // What becomes of a finished T x T piece of sums, in LDS: A or B into their
 // planes, with `mirror` at the mirrored place too, X and its planes, or the update.
 template <int STAGE, int T, int THREADS>
-__device__ __forceinline__ void finish(const OrthoArgs& a, const StepArgs& st, const Spot& s, bool mirror, float* tile)
+__device__ __forceinline__ void finish(const OrthoArgs& a, const StepArgs& st, const Spot& s, bool mirror,
+                                       const Meets<STAGE, T, THREADS>& meets, float* tile)
 {
     using Sq = Square<T>;
     const bool turned = STAGE == UPDATE && st.last && a.tall;
@@ -314,9 +343,9 @@ __device__ __forceinline__ void finish(const OrthoArgs& a, const StepArgs& st, c
         if (STAGE == GRAM || st.pair) *reinterpret_cast<uint4*>(out + at + square.low) = w.lo;
     };
     const int thread = my_thread();
-#pragma unroll 2
-    for (int t = thread; t < T * T / 8; t += THREADS) {
-        const int q = t / (T / 8), p = t % (T / 8) * 8;
+#pragma unroll
+    for (int u = 0; u < T * T / 8 / THREADS; ++u) {
+        const int t = thread + u * THREADS, q = t / (T / 8), p = t % (T / 8) * 8;
         float v[8];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -326,8 +355,8 @@ __device__ __forceinline__ void finish(const OrthoArgs& a, const StepArgs& st, c
         }
         if (STAGE == UPDATE) {
             float* at = a.x + (int64_t)s.mat * a.np * a.mp + (int64_t)(s.i0 + q) * a.mp + s.j0 + p;
-            const float4 x0 = *reinterpret_cast<const float4*>(at), x1 = *reinterpret_cast<const float4*>(at + 4);
-            const float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+            const floatx4 x0 = __builtin_bit_cast(floatx4, meets.v[u][0]), x1 = __builtin_bit_cast(floatx4, meets.v[u][1]);
+            const float x[8] = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = a.a * x[k] + v[k] * (1.f / (kB * kX));
             if (!st.last) {
@@ -342,12 +371,8 @@ __device__ __forceinline__ void finish(const OrthoArgs& a, const StepArgs& st, c
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[k] *= kA / (kX * kX);
             } else {
-                const int64_t at = square.at(s.i0 + q, s.j0 + p);
-                Pair g;
-                g.hi = *reinterpret_cast<const uint4*>(a.gram + at);
-                g.lo = *reinterpret_cast<const uint4*>(a.gram + at + square.low);
                 float x[8];
-                join(g, x);
+                join(Pair{meets.v[u][0], meets.v[u][1]}, x);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[k] = (a.b * (kB / kA)) * x[k] + (a.c * (kB / (kA * kA))) * v[k];
             }
@@ -371,31 +396,21 @@ __device__ __forceinline__ void finish(const OrthoArgs& a, const StepArgs& st, c
     }
 }
 
-template <int T>
-constexpr int kPiece = T < 128 ? T : 128;   // side of a piece that is finished at a time
-
-// A finished tile, as the matrix instructions leave it, piece by piece.
+// A finished tile, as the matrix instructions leave it.
 template <int STAGE, int T, int NWP, int NWQ, int FM, int FN>
-__device__ __forceinline__ void pieces(const OrthoArgs& a, const StepArgs& st, const Spot& s, bool mirror,
-                                       const floatx4 (&acc)[FM][FN], float* lds)
+__device__ __forceinline__ void finish_tile(const OrthoArgs& a, const StepArgs& st, const Spot& s, const floatx4 (&acc)[FM][FN],
+                                            const Meets<STAGE, T, NWP * NWQ * 64>& meets, float* lds)
 {
-    constexpr int S = kPiece<T>;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave / NWQ, wq = wave % NWQ, lane = my_thread() & 63;
-    for (int pq = 0; pq < T; pq += S)
-        for (int pp = 0; pp < T; pp += S) {
-            __syncthreads();   // every wave is done with the operands, or with the piece before
-            if (s.i0 + pq >= a.np || s.j0 + pp >= (STAGE == UPDATE ? a.mp : a.np)) continue;
+    __syncthreads();   // every wave is done with the operands
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int j = 0; j < FN; ++j) {
-                    const int q = wq * (T / NWQ) + j * 16 - pq, p = wp * (T / NWP) + i * 16 - pp;
-                    if (q >= 0 && q < S && p >= 0 && p < S)
-                        *reinterpret_cast<floatx4*>(Square<S>::chunk(lds, q + (lane & 15), p / 4 + (lane >> 4))) = acc[i][j];
-                }
-            __syncthreads();
-            finish<STAGE, S, NWP * NWQ * 64>(a, st, Spot{s.mat, s.i0 + pq, s.j0 + pp}, mirror, lds);
-        }
+        for (int j = 0; j < FN; ++j)
+            *reinterpret_cast<floatx4*>(Square<T>::chunk(lds, wq * (T / NWQ) + j * 16 + (lane & 15),
+                                                         (wp * (T / NWP) + i * 16) / 4 + (lane >> 4))) = acc[i][j];
+    __syncthreads();
+    finish<STAGE, T, NWP * NWQ * 64>(a, st, s, STAGE != UPDATE && s.i0 != s.j0, meets, lds);
 }
 
 // 32 rows of the planes of pairs, T columns from the base on, as 64 LDS lines of
@@ -433,13 +448,12 @@ template <int STAGE, bool PAIR, int T, int NWP, int NWQ, int SUB>
 __global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs a, StepArgs st)
 {
     constexpr int NW = NWP * NWQ, FM = T / NWP / 16, FN = T / NWQ / 16;
-    constexpr int S = kPiece<T>;
     constexpr int KS = PAIR ? 32 : 64;                          // reduction indices of a step
     using OP = Operand<uint16_t, T, STAGE == UPDATE, NW>;
     using OQ = Operand<uint16_t, T, false, NW>;
     constexpr int COPIES = OP::COPIES + OQ::COPIES, TILE = OP::BYTES, STEP = 2 * TILE;
     constexpr int RING = 2 * SUB;
-    __shared__ __align__(1024) char lds[RING * STEP > S * S * 4 ? RING * STEP : S * S * 4];
+    __shared__ __align__(1024) char lds[RING * STEP > T * T * 4 ? RING * STEP : T * T * 4];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave / NWQ, wq = wave % NWQ;
     const int len = (STAGE == GRAM ? a.mp : a.np) / KS;         // steps of a tile
@@ -459,6 +473,9 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs 
     if (STAGE != UPDATE) op.init(wave, 0, pld);
     const int frag_p = OP::first(wp * (T / NWP)), frag_q = OQ::first(wq * (T / NWQ));
 
+    const int nothing = a.nothing[0];
+    Meets<STAGE, T, NW * 64> meets;
+    if (T == 64 && st.split == 1) meets.load(a, st, s);
     const int vq = min(T, a.np - s.i0), vp = min(T, (STAGE == UPDATE ? a.mp : a.np) - s.j0);   // rows and columns there are
 
     const Plane xs(PAIR, s.mat, a.batch, a.np, a.mp), gs(PAIR, s.mat, a.batch, a.np, a.np);
@@ -556,7 +573,10 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs 
 #pragma unroll
             for (int j = 0; j < FN; ++j) mine[(i * FN + j) * 64] = acc[i][j];
     } else {
-        pieces<STAGE, T, NWP, NWQ>(a, st, s, STAGE != UPDATE && s.i0 != s.j0, acc, reinterpret_cast<float*>(lds));
+        if (a.batch == 1 && nothing) return;
+        // (tiles of 64 have the registers to ask for it at the start)
+        if (T > 64) meets.load(a, st, s);
+        finish_tile<STAGE, T, NWP, NWQ>(a, st, s, acc, meets, reinterpret_cast<float*>(lds));
     }
 }
 
@@ -574,6 +594,9 @@ __global__ __launch_bounds__(256) void ortho_sum_kernel(OrthoArgs a, StepArgs st
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     // fragment (i, j) of this wave's 32 x 32
     auto at = [&](int i, int j) { return wave * 256 + (i * 2 + j) * 64 + lane; };
+    const int nothing = a.nothing[0];
+    Meets<STAGE, T, 256> meets;
+    meets.load(a, st, s);
     const floatx4* sums = reinterpret_cast<const floatx4*>(a.sums) + (int64_t)tile * st.split * (T * T / 4);
     floatx4 acc[2][2] = {};
     constexpr int AHEAD = 4;   // parts whose loads are in flight
@@ -593,7 +616,8 @@ __global__ __launch_bounds__(256) void ortho_sum_kernel(OrthoArgs a, StepArgs st
 #pragma unroll
                     for (int j = 0; j < 2; ++j) acc[i][j] += v[k][i][j];
     }
-    pieces<STAGE, T, 2, 2>(a, st, s, STAGE != UPDATE && s.i0 != s.j0, acc, lds);
+    if (a.batch == 1 && nothing) return;
+    finish_tile<STAGE, T, 2, 2>(a, st, s, acc, meets, lds);
 }
 
 template <int STAGE, bool PAIR, int T, int NWP, int NWQ, int SUB>
