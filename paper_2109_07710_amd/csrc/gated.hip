@@ -18,36 +18,53 @@
 #include "tiles.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace cbw {
 namespace {
 
-// act(g) and its derivative.  The sigmoid s and its derivative s (1 - s) come
-// from exp(-|z|), so that both keep their relative accuracy far out:
-//   silu = g s(g),  silu' = s + g s (1 - s)
-//   gelu = g s(z),  gelu' = s + g s (1 - s) z',  z = 2 sqrt(2 / pi) (g + 0.044715 g^3),
-// the form with tanh, as (1 + tanh(z / 2)) / 2 = s(z).  Where g is past 110
-// in size, s (1 - s) and on the left s are zero in float32: from there on g
-// stands still in the products with them, which would else be 0 times infinity.
-// (exp in bf16: within |z| 2^-23 of itself, nothing beside the 2^-9 of what
-// is stored.)
+// act(g) and its derivative:
+//
+//   silu = g s(g),  silu' = s (1 + g (1 - s))
+//   gelu = g s(z),  gelu' = s (1 + g (1 - s) z'),  z = 2 sqrt(2 / pi) (g + 0.044715 g^3),
+//
+// the form with tanh, as (1 + tanh(z / 2)) / 2 = s(z).  s = 1 / (1 + exp(-z)) has
+// its relative accuracy at both ends; the error of 1 - s, 2^-24, is one beside 1
+// / g.  The sigmoid's own derivative would lose its accuracy in s (1 - s) and
+// comes from exp(-|g|).  Where g is past 110 in size, 1 - s and on the left s
+// are zero in float32: from there on g stands still in the products with them,
+// which would else be 0 times infinity.  (In bf16 exp is within |z| 2^-23 of
+// itself, nothing beside the 2^-9 of what is stored.)
 struct Act {
     float a, da;
 };
-template <typename T>
-__device__ __forceinline__ Act act_at(float g, int kind)
+template <typename T, int KIND>
+__device__ __forceinline__ Act act_at(float g)
 {
-    if (kind == CBW_ACT_RELU) return {g > 0.f ? g : 0.f, g > 0.f ? 1.f : 0.f};
-    constexpr float kGelu = 1.5957691216057308f;
-    const float low = g < -110.f ? -110.f : g, mid = low > 110.f ? 110.f : low;
-    const float z = kind == CBW_ACT_GELU ? kGelu * (mid + 0.044715f * mid * mid * mid) : mid;
     constexpr bool EXACT = sizeof(T) == 4;
-    const float e = EXACT ? expf(-fabsf(z)) : __expf(-fabsf(z));
-    const float r = EXACT ? 1.f / (1.f + e) : __builtin_amdgcn_rcpf(1.f + e), er = e * r;
-    const float s = z < 0.f ? er : r, ds = er * r;
-    if (kind == CBW_ACT_SIGMOID) return {s, ds};
-    const float dz = kind == CBW_ACT_GELU ? kGelu * (1.f + 0.134145f * mid * mid) : 1.f;
-    return {low * s, s + mid * ds * dz};
+    auto exponential = [](float x) { return EXACT ? expf(x) : __expf(x); };
+    auto reciprocal = [](float x) { return EXACT ? 1.f / x : __builtin_amdgcn_rcpf(x); };
+    if (KIND == CBW_ACT_RELU) return {g > 0.f ? g : 0.f, g > 0.f ? 1.f : 0.f};
+    if (KIND == CBW_ACT_SIGMOID) {
+        const float e = exponential(-fabsf(g)), r = reciprocal(1.f + e), er = e * r;
+        return {g < 0.f ? er : r, er * r};
+    }
+    constexpr float kGelu = 1.5957691216057308f;
+    const float low = g < -110.f ? -110.f : g, mid = low > 110.f ? 110.f : low, square = mid * mid;
+    const float z = KIND == CBW_ACT_GELU ? kGelu * mid * (1.f + 0.044715f * square) : mid;
+    const float s = reciprocal(1.f + exponential(-z));
+    const float slope = KIND == CBW_ACT_GELU ? mid * kGelu * (1.f + 0.134145f * square) : mid;
+    return {low * s, s * (1.f + slope * (1.f - s))};
+}
+
+// f(kind) with the activation known to the compiler.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, const F& f)
+{
+    if (act == CBW_ACT_SILU) f(std::integral_constant<int, CBW_ACT_SILU>());
+    else if (act == CBW_ACT_GELU) f(std::integral_constant<int, CBW_ACT_GELU>());
+    else if (act == CBW_ACT_SIGMOID) f(std::integral_constant<int, CBW_ACT_SIGMOID>());
+    else f(std::integral_constant<int, CBW_ACT_RELU>());
 }
 
 // I blocks of 16 features by 16 rows, as the matrix instruction leaves them (a
@@ -95,14 +112,14 @@ __device__ __forceinline__ int my_lane()
 // A tile's rows of H (or of nothing) and of the two sums or their gradients.
 struct Tensor {
     __amdgpu_buffer_rsrc_t r;
-    int64_t stride;
+    uint32_t stride;
     bool there;
 };
 template <typename T>
 __device__ __forceinline__ Tensor rows_of(const void* p, int64_t row0, int rows, int64_t stride, int cols)
 {
     const T* first = static_cast<const T*>(p) + (p ? row0 * stride : 0);
-    return {make_rsrc(first, p ? (uint32_t)(((rows - 1) * stride + cols) * (int64_t)sizeof(T)) : 0u), stride, p != nullptr};
+    return {make_rsrc(first, p ? (uint32_t)(((rows - 1) * stride + cols) * (int64_t)sizeof(T)) : 0u), (uint32_t)stride, p != nullptr};
 }
 
 // Forward: blocks 2 i and 2 i + 1 hold the gate's and the up filter's sums of
@@ -127,7 +144,7 @@ struct ForwardOut {
             const int rr = v * (64 / CHUNKS) + lane / CHUNKS, q = q0 + rr, p = p0 + lane % CHUNKS * E;
             const u32x4 w = *reinterpret_cast<const u32x4*>(Pass::at(const_cast<char*>(lds), rr, lane % CHUNKS));
             __builtin_amdgcn_raw_buffer_store_b128(
-                w, t.r, q < rows && p < K ? (uint32_t)(q * t.stride + col0 + p) * (uint32_t)sizeof(T) : kOOB, 0, 0);
+                w, t.r, q < rows && p < K ? ((uint32_t)q * t.stride + (uint32_t)(col0 + p)) * (uint32_t)sizeof(T) : kOOB, 0, 0);
         }
     }
     // v(b): the lane's four sums of block b
@@ -141,12 +158,14 @@ struct ForwardOut {
             Pass::put(lds, lane, [&](int i) { return v(2 * i + 1); });
             store(lds, lane, gu, q0, p0, K);
         }
-        Pass::put(lds, lane, [&](int i) {
-            const floatx4 g = v(2 * i), u = v(2 * i + 1);
-            floatx4 x;
+        with_act(act, [&](auto kind) {
+            Pass::put(lds, lane, [&](int i) {
+                const floatx4 g = v(2 * i), u = v(2 * i + 1);
+                floatx4 x;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) x[c] = act_at<T>(g[c], act).a * u[c];
-            return x;
+                for (int c = 0; c < 4; ++c) x[c] = act_at<T, decltype(kind)::value>(g[c]).a * u[c];
+                return x;
+            });
         });
         store(lds, lane, h, q0, p0, 0);
     }
@@ -173,9 +192,9 @@ struct BackwardOut {
     struct Ahead {
         uint4 g[VECS], u[VECS];
     };
-    __device__ __forceinline__ uint32_t place(int64_t stride, int q, int p, int col0) const
+    __device__ __forceinline__ uint32_t place(uint32_t stride, int q, int p, int col0) const
     {
-        return q < rows && p < K ? (uint32_t)(q * stride + col0 + p) * (uint32_t)sizeof(T) : kOOB;
+        return q < rows && p < K ? ((uint32_t)q * stride + (uint32_t)(col0 + p)) * (uint32_t)sizeof(T) : kOOB;
     }
     __device__ __forceinline__ void load(Ahead& x, int q0, int p0) const
     {
@@ -206,6 +225,11 @@ struct BackwardOut {
     {
         const int lane = my_lane();
         Pass::put(lds, lane, v);
+        with_act(act, [&](auto kind) { meet<decltype(kind)::value>(lds, lane, q0, p0, x); });
+    }
+    template <int ACT>
+    __device__ __forceinline__ void meet(char* lds, int lane, int q0, int p0, const Ahead& x) const
+    {
 #pragma unroll
         for (int t = 0; t < VECS; ++t) {
             const int rr = t * (64 / LANES) + lane / LANES, q = q0 + rr, p = p0 + lane % LANES * E;
@@ -220,7 +244,7 @@ struct BackwardOut {
             expand(x.u[t], u);
 #pragma unroll
             for (int k = 0; k < E; ++k) {
-                const Act f = act_at<T>(g[k], act);
+                const Act f = act_at<T, ACT>(g[k]);
                 dg[k] = d[k] * u[k] * f.da;
                 du[k] = d[k] * f.a;
                 hh[k] = f.a * u[k];

@@ -642,7 +642,7 @@ hipError_t launch_product(const OrthoArgs& a, const StepArgs& st, const OrthoDea
         if (d.tiles > CBW_NUM_CUS) return launch_tiles<STAGE, PAIR, 128, 2, 2, 1>(a, st, d, s);
         return launch_tiles<STAGE, PAIR, 128, 2, 4, 2>(a, st, d, s);
     default:
-        if (d.tiles * d.split > CBW_NUM_CUS) return launch_tiles<STAGE, PAIR, 64, 2, 2, 1>(a, st, d, s);
+        if (d.tiles * d.split > 2 * CBW_NUM_CUS) return launch_tiles<STAGE, PAIR, 64, 2, 2, 1>(a, st, d, s);
         return launch_tiles<STAGE, PAIR, 64, 2, 2, 2>(a, st, d, s);
     }
 }
