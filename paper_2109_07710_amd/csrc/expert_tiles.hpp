@@ -211,7 +211,7 @@ struct Operand {
     template <int F>
     static __device__ __forceinline__ void fragments(const char* lds, int at, int ks, uint4 (&f)[F])
     {
-        static_assert((F & (F - 1)) == 0, "a power of two");
+        static_assert(!ACROSS || (F & (F - 1)) == 0, "a power of two");
         asm volatile("" : "+v"(at));   // (not to be worked out ahead for every block)
 #pragma unroll
         for (int i = 0; i < F; ++i) {

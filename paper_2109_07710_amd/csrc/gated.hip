@@ -109,6 +109,12 @@ __device__ __forceinline__ int my_lane()
     return lane;
 }
 
+// How a kernel's outputs go to memory: what the tiled ones write would push the
+// operands out of the L2 and goes past it (16384 rows, 2048 -> 4096, us: forward
+// 532 for 543 to 555, backward 365 for 368).  The streaming ones' few rows stay
+// at hand.
+enum { NEAR = 0, PAST = 2 };
+
 // A tile's rows of H (or of nothing) and of the two sums or their gradients.
 struct Tensor {
     __amdgpu_buffer_rsrc_t r;
@@ -124,7 +130,7 @@ __device__ __forceinline__ Tensor rows_of(const void* p, int64_t row0, int rows,
 
 // Forward: blocks 2 i and 2 i + 1 hold the gate's and the up filter's sums of
 // the same 16 features; rows q0 .. q0 + 15 of the tile, features p0 on.
-template <typename T, int I>
+template <typename T, int I, int WAY>
 struct ForwardOut {
     using Pass = Passage<T, I>;
     static constexpr int BYTES = Pass::BYTES;
@@ -144,7 +150,7 @@ struct ForwardOut {
             const int rr = v * (64 / CHUNKS) + lane / CHUNKS, q = q0 + rr, p = p0 + lane % CHUNKS * E;
             const u32x4 w = *reinterpret_cast<const u32x4*>(Pass::at(const_cast<char*>(lds), rr, lane % CHUNKS));
             __builtin_amdgcn_raw_buffer_store_b128(
-                w, t.r, q < rows && p < K ? ((uint32_t)q * t.stride + (uint32_t)(col0 + p)) * (uint32_t)sizeof(T) : kOOB, 0, 0);
+                w, t.r, q < rows && p < K ? ((uint32_t)q * t.stride + (uint32_t)(col0 + p)) * (uint32_t)sizeof(T) : kOOB, 0, WAY);
         }
     }
     // v(b): the lane's four sums of block b
@@ -174,7 +180,7 @@ struct ForwardOut {
 // Backward: I blocks of dH (in float32 through the LDS, 16 rows) meet g and u,
 // which are loaded ahead.  dg and du may lie where g and u did: a lane has read
 // its own before it writes them.
-template <typename T, int I>
+template <typename T, int I, int WAY>
 struct BackwardOut {
     using Pass = Passage<float, I>;
     static constexpr int BYTES = Pass::BYTES, E = 16 / (int)sizeof(T);
@@ -249,9 +255,9 @@ struct BackwardOut {
                 du[k] = d[k] * f.a;
                 hh[k] = f.a * u[k];
             }
-            __builtin_amdgcn_raw_buffer_store_b128(narrow(dg), dgu.r, place(dgu.stride, q, p, 0), 0, 0);
-            __builtin_amdgcn_raw_buffer_store_b128(narrow(du), dgu.r, place(dgu.stride, q, p, K), 0, 0);
-            if (h.there) __builtin_amdgcn_raw_buffer_store_b128(narrow(hh), h.r, place(h.stride, q, p, 0), 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(narrow(dg), dgu.r, place(dgu.stride, q, p, 0), 0, WAY);
+            __builtin_amdgcn_raw_buffer_store_b128(narrow(du), dgu.r, place(dgu.stride, q, p, K), 0, WAY);
+            if (h.there) __builtin_amdgcn_raw_buffer_store_b128(narrow(hh), h.r, place(h.stride, q, p, 0), 0, WAY);
         }
     }
 };
@@ -314,14 +320,17 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void gated_kernel(GatedArgs a)
     using OQ = typename Tl::OQ;
     constexpr int KB = Tl::KB, COPIES = Tl::COPIES, FEATURES = Tl::FEATURES;
     constexpr int BI = FM < 4 ? FM : 4;   // blocks of dH that pass the LDS at a time
-    using Forward = ForwardOut<T, BACK ? 4 : FM / 2>;
-    using Backward = BackwardOut<T, BI>;
+    using Forward = ForwardOut<T, BACK ? 4 : FM / 2, PAST>;
+    using Backward = BackwardOut<T, BI, PAST>;
     __shared__ __align__(1024) char lds_p[2][OP::BYTES];
     __shared__ __align__(1024) char lds_q[2][OQ::BYTES];
     __shared__ __align__(1024) char lds_out[NW][BACK ? Backward::BYTES : Forward::BYTES];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wp = wave / NWQ, wq = wave % NWQ;
+    // A CU's four SIMDs take the waves in turn: each has rows of both halves, so
+    // that a tile of half its rows, whose other waves have nothing to multiply,
+    // takes half the time.
+    const int wp = wave % NWP, wq = wave / NWP;
     struct Tile {
         int e, p0, qrows;
         int64_t row0;
@@ -398,6 +407,15 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void gated_kernel(GatedArgs a)
         if (steps > 1) wait_copies<COPIES>();
         else wait_copies<0>();
         barrier();
+        if (wq * (TQ / NWQ) >= t.qrows) {
+            // none of the wave's rows are there: it copies
+            for (int s = 0; s < steps; ++s) {
+                wait_copies<0>();
+                barrier();
+                if (s + 2 < steps) copy((s + 2) * KB, s & 1);
+            }
+            return;
+        }
         read(fa, 0, 0);
         for (int s = 0; s < steps; ++s) {
             const int buf = s & 1;
@@ -424,7 +442,9 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void gated_kernel(GatedArgs a)
             start(next);
         }
         const int q0 = wq * (TQ / NWQ), p0 = t.p0 + wp * (FEATURES / NWP);
-        if constexpr (BACK) {
+        if (q0 >= t.qrows) {
+            // (nothing to store)
+        } else if constexpr (BACK) {
             const Backward out(a, t.row0, t.qrows);
             constexpr int H = FM / BI, N = FN * H;
             typename Backward::Ahead x[2];
@@ -457,8 +477,8 @@ __global__ __launch_bounds__(NW * 64) void gated_stream_kernel(GatedArgs a)
     using OP = typename Tl::OP;
     using OQ = typename Tl::OQ;
     constexpr int KB = Tl::KB, COPIES = Tl::COPIES, FEATURES = Tl::FEATURES, STAGE = OP::BYTES + OQ::BYTES;
-    using Forward = ForwardOut<T, BACK ? 4 : FM / 2>;
-    using Backward = BackwardOut<T, BACK ? FM : 4>;
+    using Forward = ForwardOut<T, BACK ? 4 : FM / 2, NEAR>;
+    using Backward = BackwardOut<T, BACK ? FM : 4, NEAR>;
     constexpr int SUMS = NW * FM * FN * 1024, OUT = BACK ? Backward::BYTES : Forward::BYTES;
     __shared__ __align__(1024) char lds[NW * RING * STAGE > SUMS + FN * OUT ? NW * RING * STAGE : SUMS + FN * OUT];
 
@@ -593,7 +613,14 @@ hipError_t launch(const GatedArgs& a, hipStream_t s)
     constexpr int W = BACK ? 1 : 2;   // lines of the filters to a feature
     const int64_t mean = a.rows / std::max<int64_t>(1, std::min<int64_t>(a.E, a.rows));
     if constexpr (BF16) {
-        if (mean >= 160 && likely_tiles(a, 256, 256 / W) >= 200) return launch_tiles<T, BACK, 256, 256, 2, 4>(a, s);
+        if (mean >= 160 && likely_tiles(a, 256, 256 / W) >= 200) {
+            // 192 rows take 0.8 of the time of 256, and where that fills the last turn
+            // of the workgroups better, less in all (4099 rows, 1024 -> 2816, 374 tiles
+            // or 484, us: 50.9 for 55.6; 16384 rows, 2048 -> 4096, turns alike: 582 for 551)
+            auto turns = [&](int rows) { return (likely_tiles(a, rows, 256 / W) + CBW_NUM_CUS - 1) / CBW_NUM_CUS; };
+            if (4 * turns(192) < 5 * turns(256)) return launch_tiles<T, BACK, 256, 192, 2, 4>(a, s);
+            return launch_tiles<T, BACK, 256, 256, 2, 4>(a, s);
+        }
         if (mean > 16 && likely_tiles(a, 128, 128 / W) >= 200) return launch_tiles<T, BACK, 128, 128, 2, 2>(a, s);
         if (mean > 64) return launch_stream<T, BACK, 64, 4, 4, 2>(a, s);
     } else {

@@ -80,6 +80,8 @@ LARGE = [
     (4, 9000, 64, 2064, "bf16"),
     (4, 9000, 72, 4104, "bf16"),
     (5, 8000, 264, 2128, "bf16"),
+    (2, 4000, 72, 4104, "bf16"),       # tiles of 192 rows
+    (3, 4100, 136, 4104, "bf16"),
     (20, 2000, 200, 2056, "bf16"),     # tiles of 128 rows
     (20, 2000, 136, 4104, "bf16"),
     (3, 2000, 1032, 264, "bf16"),      # few tiles: rows by 64
