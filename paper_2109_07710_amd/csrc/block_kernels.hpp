@@ -209,6 +209,7 @@ struct StepArgs {
     int from;                   // which of the planes holds X
     int split;                  // workgroups that share a tile's reduction
     bool last, pair, next_pair;
+    bool quarters;              // those of the 256 x 256 tiles that do not fill a turn
 };
 struct PanelArgs {
     int width, panels, from;    // which of the two sets of A's parts is read

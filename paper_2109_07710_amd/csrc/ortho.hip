@@ -276,7 +276,21 @@ __device__ __forceinline__ Spot spot_of(const OrthoArgs& a, const Tiles& tiles, 
         s.i0 = (4 * b + i) * T;
         s.j0 = j * T;
     }
+    // (the same in all lanes, which divisions hide)
+    s.mat = __builtin_amdgcn_readfirstlane(s.mat);
+    s.i0 = __builtin_amdgcn_readfirstlane(s.i0);
+    s.j0 = __builtin_amdgcn_readfirstlane(s.j0);
     return s;
+}
+
+// How many of `count` tiles of 256 go as such, one to a CU at a time: whole
+// turns of all CUs, and a last one that is nearly whole.  The rest go by
+// quarters, two to a CU.
+constexpr int kLeft = 199;   // (a turn of such tiles takes some 0.8 of a turn of as many quarters)
+__device__ __forceinline__ int large_tiles(int count)
+{
+    const int rest = count % CBW_NUM_CUS;
+    return rest > kLeft ? count : count - rest;
 }
 
 // A tile in LDS as [row][column], in float32.  A row's 16-byte chunks are moved
@@ -435,8 +449,72 @@ struct PairsAcross {
     }
 };
 
-// T x T tiles by NWP x NWQ waves.  A step is 128 bytes of reduction indices of
-// both operands: 64 high parts, or 32 pairs.  SUB of them go from one barrier to
+// A tile's operands, as they come into LDS: from step `first` on.  A step is 128
+// bytes of reduction indices of both: 64 high parts, or 32 pairs.
+template <int STAGE, bool PAIR, int T, int NW>
+struct Feed {
+    static constexpr int KS = PAIR ? 32 : 64;                   // reduction indices of a step
+    using OP = Operand<uint16_t, T, STAGE == UPDATE, NW>;
+    using OQ = Operand<uint16_t, T, false, NW>;
+    static constexpr int COPIES = OP::COPIES + OQ::COPIES, TILE = OP::BYTES, STEP = 2 * TILE;
+    OP op;
+    OQ oq;
+    PairsAcross<T, NW> across;
+    const _Float16 *pb, *qb;
+    int64_t pld, qld;
+    int first, vp, vq;   // columns and rows there are
+
+    __device__ __forceinline__ Feed(const OrthoArgs& a, const StepArgs& st, const Spot& s, int wave, int at) : first(at)
+    {
+        pld = (STAGE == SQUARE ? a.np : a.mp) * (PAIR ? 2 : 1);
+        qld = (STAGE == GRAM ? a.mp : a.np) * (PAIR ? 2 : 1);
+        vq = min(T, a.np - s.i0);
+        vp = min(T, (STAGE == UPDATE ? a.mp : a.np) - s.j0);
+        const Plane xs(PAIR, s.mat, a.batch, a.np, a.mp), gs(PAIR, s.mat, a.batch, a.np, a.np);
+        const _Float16* x = a.planes[st.from];
+        pb = STAGE == GRAM ? x + xs.at(s.j0, 0) : STAGE == SQUARE ? a.gram + gs.at(s.j0, 0) : x + xs.at(0, s.j0);
+        qb = STAGE == GRAM ? x + xs.at(s.i0, 0) : STAGE == SQUARE ? a.gram + gs.at(s.i0, 0) : a.poly + gs.at(s.i0, 0);
+        pb = uniform(pb);
+        qb = uniform(qb);
+        oq.init(wave, 0, qld);
+        if (STAGE != UPDATE) op.init(wave, 0, pld);
+        else if (PAIR) across.init(wave, vp, a.mp);
+        else op.init(wave, vp, pld);
+    }
+    static __device__ __forceinline__ const _Float16* uniform(const _Float16* p)
+    {
+        const uint64_t a = reinterpret_cast<uint64_t>(p);
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((int)a), hi = __builtin_amdgcn_readfirstlane((int)(a >> 32));
+        return reinterpret_cast<const _Float16*>((uint64_t)hi << 32 | lo);
+    }
+    // The same, with offsets that the compiler takes for new ones: it would work
+    // out those of all copies ahead and fill registers.
+    __device__ __forceinline__ Feed here() const
+    {
+        Feed f = *this;
+        auto hold = [](auto& o) {
+#pragma unroll
+            for (int j = 0; j < (int)(sizeof(o.off) / 4); ++j) asm volatile("" : "+v"(o.off[j]));
+        };
+        hold(f.op);
+        hold(f.oq);
+        return f;
+    }
+    __device__ __forceinline__ void copy(int wave, int step, char* to) const
+    {
+        const int64_t k = first + step;
+        if (STAGE == UPDATE) {
+            const u32x4_t r = make_rsrc_words(pb + k * KS * pld, (uint32_t)(((KS - 1) * pld + vp * (PAIR ? 2 : 1)) * 2));
+            if (PAIR) across.copy(wave, r, to);
+            else op.copy(wave, r, 0, 0, to);
+        } else {
+            op.copy(wave, make_rsrc_words(pb + k * 64, (uint32_t)(((vp - 1) * pld + 64) * 2)), 0, 64, to);
+        }
+        oq.copy(wave, make_rsrc_words(qb + k * 64, (uint32_t)(((vq - 1) * qld + 64) * 2)), 0, 64, to + TILE);
+    }
+};
+
+// T x T tiles by NWP x NWQ waves.  SUB of them go from one barrier to
 // the next, and as many again are on their way into LDS meanwhile.
 //
 // The steps of a tile are shared out to st.split workgroups, whose sums go to
@@ -448,56 +526,38 @@ template <int STAGE, bool PAIR, int T, int NWP, int NWQ, int SUB>
 __global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs a, StepArgs st)
 {
     constexpr int NW = NWP * NWQ, FM = T / NWP / 16, FN = T / NWQ / 16;
-    constexpr int KS = PAIR ? 32 : 64;                          // reduction indices of a step
-    using OP = Operand<uint16_t, T, STAGE == UPDATE, NW>;
-    using OQ = Operand<uint16_t, T, false, NW>;
-    constexpr int COPIES = OP::COPIES + OQ::COPIES, TILE = OP::BYTES, STEP = 2 * TILE;
+    using Fd = Feed<STAGE, PAIR, T, NW>;
+    using OP = typename Fd::OP;
+    using OQ = typename Fd::OQ;
+    constexpr int KS = Fd::KS, COPIES = Fd::COPIES, TILE = Fd::TILE, STEP = Fd::STEP;
     constexpr int RING = 2 * SUB;
     __shared__ __align__(1024) char lds[RING * STEP > T * T * 4 ? RING * STEP : T * T * 4];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave / NWQ, wq = wave % NWQ;
     const int len = (STAGE == GRAM ? a.mp : a.np) / KS;         // steps of a tile
-    const Tiles tiles = tiles_of<STAGE, T>(a);
-    const int units = tiles.count * st.split;
+    const bool quarters = STAGE != UPDATE && T == 128 && st.quarters;
+    const Tiles tiles = quarters ? tiles_of<STAGE, 256>(a) : tiles_of<STAGE, T>(a);
+    const int taken = quarters ? large_tiles(tiles.count) : 0;
+    const int units = quarters ? (tiles.count - taken) * 4 : tiles.count * st.split;
     if ((int)blockIdx.x >= units) return;
-    const int me = xcd_remap(blockIdx.x, units), tile = me / st.split, part = me - tile * st.split;
+    const int me = xcd_remap(blockIdx.x, units), tile = quarters ? taken + me / 4 : me / st.split;
+    const int part = quarters ? 0 : me - tile * st.split;
     const int first = (int)((int64_t)part * len / st.split), steps = (int)((int64_t)(part + 1) * len / st.split) - first;
-    const Spot s = spot_of<STAGE, T>(a, tiles, tile);
+    Spot s = quarters ? spot_of<STAGE, 256>(a, tiles, tile) : spot_of<STAGE, T>(a, tiles, tile);
+    if (quarters) {
+        s.i0 += me % 4 / 2 * T;
+        s.j0 += me % 2 * T;
+        if (s.i0 >= a.np || s.j0 > s.i0) return;
+    }
     if (!tiles.listed && a.nothing[s.mat] != 0) return;
 
-    OP op;
-    OQ oq;
-    PairsAcross<T, NW> across;
-    const int64_t pld = (STAGE == SQUARE ? a.np : a.mp) * (PAIR ? 2 : 1), qld = (STAGE == GRAM ? a.mp : a.np) * (PAIR ? 2 : 1);
-    oq.init(wave, 0, qld);
-    if (STAGE != UPDATE) op.init(wave, 0, pld);
     const int frag_p = OP::first(wp * (T / NWP)), frag_q = OQ::first(wq * (T / NWQ));
 
     const int nothing = a.nothing[0];
     Meets<STAGE, T, NW * 64> meets;
     if (T == 64 && st.split == 1) meets.load(a, st, s);
-    const int vq = min(T, a.np - s.i0), vp = min(T, (STAGE == UPDATE ? a.mp : a.np) - s.j0);   // rows and columns there are
-
-    const Plane xs(PAIR, s.mat, a.batch, a.np, a.mp), gs(PAIR, s.mat, a.batch, a.np, a.np);
-    const _Float16* x = a.planes[st.from];
-    const _Float16* pb = STAGE == GRAM ? x + xs.at(s.j0, 0) : STAGE == SQUARE ? a.gram + gs.at(s.j0, 0) : x + xs.at(0, s.j0);
-    const _Float16* qb = STAGE == GRAM ? x + xs.at(s.i0, 0) : STAGE == SQUARE ? a.gram + gs.at(s.i0, 0) : a.poly + gs.at(s.i0, 0);
-    if (STAGE == UPDATE) {
-        if (PAIR) across.init(wave, vp, a.mp);
-        else op.init(wave, vp, pld);
-    }
-    auto copy = [&](int step) {
-        char* to = lds + step % RING * STEP;
-        const int64_t k = first + step;
-        if (STAGE == UPDATE) {
-            const u32x4_t r = make_rsrc_words(pb + k * KS * pld, (uint32_t)(((KS - 1) * pld + vp * (PAIR ? 2 : 1)) * 2));
-            if (PAIR) across.copy(wave, r, to);
-            else op.copy(wave, r, 0, 0, to);
-        } else {
-            op.copy(wave, make_rsrc_words(pb + k * 64, (uint32_t)(((vp - 1) * pld + 64) * 2)), 0, 64, to);
-        }
-        oq.copy(wave, make_rsrc_words(qb + k * 64, (uint32_t)(((vq - 1) * qld + 64) * 2)), 0, 64, to + TILE);
-    };
+    const Fd feed(a, st, s, wave, first);
+    auto copy = [&](int step) { feed.copy(wave, step, lds + step % RING * STEP); };
 
     floatx4 acc[FM][FN];
 #pragma unroll
@@ -580,6 +640,116 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs 
     }
 }
 
+// A and A A of large batches: 256 x 256 tiles by eight waves, two buffers of a
+// step.  A wave's 64 x 128 sums leave registers for two sets of fragments,
+// which take turns:
+//
+//   pairs        hi hi (meanwhile the low parts are read), lo hi, and behind the
+//                barrier hi lo (and the next step's high parts, into the sets
+//                that are free: those of the columns change places each step)
+//   high parts   the halves of a step, the barrier between them
+//
+// (7 of 8 matrices 4096 x 2048, us, tiles of 128 and of 256: A on pairs 358 and
+// 284, on high parts 162 and 121, A A 191 and 160, 90 and 74.  B X gained
+// nothing, 344 and 353 on high parts, 686 and 682 on pairs: half of its time
+// goes into reading and writing X.)
+template <int STAGE, bool PAIR>
+__global__ __launch_bounds__(512) void ortho_large_kernel(OrthoArgs a, StepArgs st)
+{
+    static_assert(STAGE != UPDATE, "see above");
+    constexpr int T = 256, NWQ = 4, FM = 8, FN = 4;
+    using Fd = Feed<STAGE, PAIR, T, 8>;
+    using OP = typename Fd::OP;
+    using OQ = typename Fd::OQ;
+    __shared__ __align__(1024) char lds[2 * Fd::STEP];
+    static_assert(sizeof(lds) >= 128 * 128 * 4, "a quarter of a finished tile");
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave / NWQ, wq = wave % NWQ;
+    const int steps = (STAGE == GRAM ? a.mp : a.np) / Fd::KS;   // an even number: sizes are multiples of 128
+    const Tiles tiles = tiles_of<STAGE, T>(a);
+    const int count = large_tiles(tiles.count);
+    if ((int)blockIdx.x >= count) return;
+    const Spot s = spot_of<STAGE, T>(a, tiles, xcd_remap(blockIdx.x, count));
+    if ((a.batch == 1 || !tiles.listed) && a.nothing[s.mat] != 0) return;
+    const int frag_p = OP::first(wp * (T / 2)), frag_q = OQ::first(wq * (T / NWQ));
+    const Fd feed(a, st, s, wave, 0);
+    auto copy = [&](const Fd& f, int step) { f.copy(wave, step, lds + (step & 1) * Fd::STEP); };
+
+    floatx4 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    uint4 p[2][FM], q[2][FN];
+    auto read = [&](int buf, int half, int to_p, int to_q) {
+        const char* at = lds + buf * Fd::STEP;
+        OQ::fragments(at + Fd::TILE, frag_q, half, q[to_q]);
+        OP::fragments(at, frag_p, half, p[to_p]);
+    };
+    auto multiply = [&](int of_p, int of_q) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = mfma_half(acc[i][j], p[of_p][i], q[of_q][j]);
+    };
+    auto interleave = [&]() {
+        constexpr int READS = FM + FN, MUL = FM * FN;
+#pragma unroll
+        for (int i = 0; i < READS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                    // an LDS read
+            __builtin_amdgcn_sched_group_barrier(0x008, MUL / READS, 0);          // matrix instructions
+        }
+    };
+    copy(feed.here(), 0);
+    copy(feed.here(), 1);
+    wait_copies<Fd::COPIES>();
+    barrier();
+    read(0, 0, 0, 0);
+    for (int k0 = 0; k0 < steps; k0 += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int k = k0 + u, hi = PAIR ? u : 0;
+            read(u, 1, hi ^ 1, 1);
+            multiply(hi, 0);
+            interleave();
+            if (PAIR) {
+                multiply(hi ^ 1, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const Fd next = feed.here();
+            wait_copies<0>();
+            wait_reads();
+            barrier();
+            if (k + 2 < steps) copy(next, k + 2);
+            read(u ^ 1, 0, PAIR ? hi ^ 1 : 0, 0);   // (after the last step: what was there, unused)
+            multiply(PAIR ? hi : 1, 1);
+            interleave();
+            __builtin_amdgcn_sched_barrier(0);   // (the next reads have no registers yet)
+        }
+    }
+    wait_reads();
+    float* tile = reinterpret_cast<float*>(lds);   // a quarter at a time
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const int hq = n >> 1, hp = n & 1;
+        const Spot part{s.mat, s.i0 + hq * 128, s.j0 + hp * 128};
+        if (part.i0 >= a.np || part.j0 > part.i0) continue;   // (past the matrix; the mirrored quarter's)
+        Meets<STAGE, 128, 512> meets;
+        meets.load(a, st, part);
+        __syncthreads();   // every wave is done with the operands, or the quarter before
+        if (wp == hp && wq >> 1 == hq) {
+            const int lane = my_thread() & 63;
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    *reinterpret_cast<floatx4*>(Square<128>::chunk(tile, (wq & 1) * 64 + j * 16 + (lane & 15), i * 4 + (lane >> 4))) = acc[i][j];
+        }
+        __syncthreads();
+        finish<STAGE, 128, 512>(a, st, part, part.i0 != part.j0, meets, tile);
+    }
+}
+
 // The parts of split tiles of 64 x 64, added in order, and what becomes of them.
 template <int STAGE>
 __global__ __launch_bounds__(256) void ortho_sum_kernel(OrthoArgs a, StepArgs st)
@@ -635,6 +805,16 @@ template <int STAGE, bool PAIR>
 hipError_t launch_product(const OrthoArgs& a, const StepArgs& st, const OrthoDeal& d, hipStream_t s)
 {
     switch (d.side) {
+    case 256:
+        if constexpr (STAGE != UPDATE) {
+            // (how many there are without the matrices of zeros, the kernels find)
+            ortho_large_kernel<STAGE, PAIR><<<d.tiles, 512, 0, s>>>(a, st);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            StepArgs rest = st;
+            rest.quarters = true;
+            return launch_tiles<STAGE, PAIR, 128, 2, 2, 1>(a, rest, {128, 4 * std::min(d.tiles, kLeft), 1}, s);
+        }
     case 128:
         // two workgroups to a CU where there are as many, else twice the steps to a
         // barrier and twice the waves (2048 x 2048, A | A A | B X, us: 25 | 25 | 31 for
@@ -664,11 +844,11 @@ int64_t round_up(int64_t v, int64_t by) { return (v + by - 1) / by * by; }
 // parts of a split one 2 beside their steps, and the launch that adds them up
 // 3.5 and 0.25 a part (us, 3 x 333 x 1001 and 256 x 2304, measured by launches).
 template <typename F>
-OrthoDeal deal(F tiles, int64_t len, bool pair, bool by128)
+OrthoDeal deal(F tiles, int64_t len, bool pair, bool by128, bool by256)
 {
     OrthoDeal d{};
     // (those of 128 are finished whole: both sides are filled up to that)
-    d.side = by128 && tiles(128) >= 128 ? 128 : 64;
+    d.side = by256 && tiles(256) > kLeft ? 256 : by128 && tiles(128) >= 128 ? 128 : 64;
     d.tiles = (int)tiles(d.side);
     d.split = 1;
     const int64_t steps = len / (pair ? 32 : 64);
@@ -704,7 +884,8 @@ OrthoPlan ortho_plan(const cbw_ortho_desc* d)
                 return d->batch * (k == UPDATE ? rows * cols : rows * (rows + 1) / 2);
             };
             OrthoDeal& e = p.deal[pair][k];
-            e = deal(tiles, k == GRAM ? p.mp : p.np, pair, p.np % 128 == 0 && p.mp % 128 == 0);
+            const bool by128 = p.np % 128 == 0 && p.mp % 128 == 0;
+            e = deal(tiles, k == GRAM ? p.mp : p.np, pair, by128, by128 && k != UPDATE);
             if (e.split > 1) sums = std::max(sums, (size_t)e.tiles * e.split * e.side * e.side * 4);
         }
     }

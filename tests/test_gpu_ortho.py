@@ -65,6 +65,26 @@ def test_large():
         ref.check(_run(m.transpose(1, 2).contiguous(), out)[0], m[0].t(), QUINTIC, 5, 1e-7, out + " tall")
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(640, 900), (1100, 600)])
+def test_large_batch(rows, cols, out):
+    """Enough for tiles of 256, the last ones half empty; one matrix of zeros."""
+    batch = 44
+    m = _draw(1, rows, cols, 7) * torch.linspace(0.5, 2.0, batch)[:, None, None]
+    m[1::2] = m[1::2].flip(2)
+    m[9] = 0.0
+    o = _run(m, out)
+    assert bool((o[9] == 0).all())
+    for i in (0, 1, 43):
+        ref.check(o[i], m[i], QUINTIC, 5, 1e-7, "matrix %d" % i)
+    # the others are the same matrices at other sizes, which the norm takes off but for eps and its rounding
+    for i in range(2, batch):
+        if i != 9:
+            off = float((o[i].double() - o[i & 1].double()).norm() / o[i & 1].double().norm())
+            assert off <= (2.0 ** -7 if out == "bf16" else 2.0 ** -16), (i, off)
+    assert torch.equal(o, _run(m, out)), "the same call, the same bits"
+
+
 def test_becomes_orthogonal():
     """Cubic steps converge: X X^T = I to the last step's own error.  Its products, 96 long, are off by 8e-7 an entry (R is below
     0.1) and dA by 2e-6 more on the diagonal (see ortho_ref); dA enters X X^T once, d(B X) twice through a row of 96 values:
