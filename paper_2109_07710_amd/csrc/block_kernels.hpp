@@ -198,7 +198,7 @@ struct OrthoArgs {
     bool in_f32, out_f32, tall;
     float a, b, c;
     double eps;
-    double* partial;            // [batch][parts]
+    double* partial;            // [batch][parts], or [batch][panels]
     int* nothing;               // [batch]: a matrix of zeros
     float* x;                   // [batch][np][mp]
     _Float16* planes[2];        // of X, two sets in turn
@@ -213,9 +213,8 @@ struct StepArgs {
 };
 struct PanelArgs {
     int width, panels, from;    // which of the two sets of A's parts is read
-    bool last;
+    bool first, last;
 };
-hipError_t launch_ortho_norm(const OrthoArgs& a, hipStream_t s);
 hipError_t launch_ortho_narrow(const OrthoArgs& a, const OrthoPlan& p, int steps, hipStream_t s);
 hipError_t launch_orthogonalize(const OrthoArgs& a, const OrthoPlan& p, int steps, hipStream_t s);
 

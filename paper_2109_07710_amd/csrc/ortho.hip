@@ -120,6 +120,16 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(OrthoArgs a)
     if (threadIdx.x == 0) a.partial[(int64_t)mat * a.parts + z] = sums[0] + sums[1] + sums[2] + sums[3];
 }
 
+// 1 / (|M| + eps) from the parts of the sum; called by whole waves.
+__device__ __forceinline__ double inverse_norm(const OrthoArgs& a, int mat, bool& nothing)
+{
+    double s = 0.0;
+    for (int z = threadIdx.x & 63; z < a.parts; z += 64) s += a.partial[(int64_t)mat * a.parts + z];
+    for (int k = 32; k >= 1; k >>= 1) s += __shfl_xor(s, k);
+    nothing = s == 0.0;
+    return inverse_of(s, a.eps);
+}
+
 // Where a matrix's planes of `ld` columns and `rows` rows (of one matrix) hold
 // the high part of (i, j), and how much further its low part lies.  Products
 // on pairs find 32 high parts and the same columns' 32 low parts in each 128
@@ -873,7 +883,7 @@ OrthoPlan ortho_plan(const cbw_ortho_desc* d)
     p.np = (int)round_up(n, n > 256 ? 128 : 64);
     p.mp = (int)round_up(m, n > 256 ? 128 : 64);
     // steps on high parts: see above (n itself, not what it is filled up to)
-    if (d->out_dtype == CBW_BF16)
+    if (d->out_dtype == CBW_BF16 && d->a >= 1.f)   // (below 1 small values never grow, and never get their last steps)
         for (double g = 1.0; p.coarse + 2 < d->steps && g <= 0.14 * (double)n; g *= (double)d->a * d->a) ++p.coarse;
     p.parts = (int)std::min<int64_t>(512, std::max<int64_t>(1, (int64_t)d->rows * d->cols / 8192));
     size_t sums = 0;
@@ -904,17 +914,12 @@ OrthoPlan ortho_plan(const cbw_ortho_desc* d)
     return p;
 }
 
-hipError_t launch_ortho_norm(const OrthoArgs& a, hipStream_t s)
-{
-    ortho_norm_kernel<<<a.batch * a.parts, 256, 0, s>>>(a);
-    return hipGetLastError();
-}
-
 hipError_t launch_orthogonalize(const OrthoArgs& a, const OrthoPlan& p, int steps, hipStream_t s)
 {
     if (p.rows) return launch_ortho_narrow(a, p, steps, s);
     auto pair = [&](int k) { return k >= p.coarse; };
-    hipError_t e = launch_ortho_norm(a, s);
+    ortho_norm_kernel<<<a.batch * a.parts, 256, 0, s>>>(a);
+    hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     ortho_start_kernel<<<a.batch * (a.np / 64) * (a.mp / 64), 256, 0, s>>>(a, pair(0));
     if ((e = hipGetLastError()) != hipSuccess) return e;

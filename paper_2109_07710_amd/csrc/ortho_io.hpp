@@ -33,15 +33,6 @@ __device__ __forceinline__ double inverse_of(double sum, double eps)
     const double norm = sqrt(sum), all = norm + eps;
     return all > 0.0 ? (norm < __builtin_inf() ? 1.0 / all : __builtin_nan("")) : all == 0.0 ? 0.0 : all;
 }
-// The same from the parts of the sum; called by whole waves.
-__device__ __forceinline__ double inverse_norm(const OrthoArgs& a, int mat, bool& nothing)
-{
-    double s = 0.0;
-    for (int z = threadIdx.x & 63; z < a.parts; z += 64) s += a.partial[(int64_t)mat * a.parts + z];
-    for (int k = 32; k >= 1; k >>= 1) s += __shfl_xor(s, k);
-    nothing = s == 0.0;
-    return inverse_of(s, a.eps);
-}
 
 // Eight values of a row of the output, from column `col` on.
 __device__ __forceinline__ void store_out(const OrthoArgs& a, int mat, int row, int col, const float (&v)[8])

@@ -7,8 +7,10 @@
 //   A = the panels' sums of x x^T,  B = b A + c A A,  x = a x + B x
 //
 // A launch a step: every workgroup adds up the panels' parts of A itself, in
-// order, and leaves its own part of the next one.  Matrices of one panel take
-// one launch in all, from the norm to the update.  What bounds it are launches
+// order, and leaves its own part of the next one.  The launch before them takes
+// every panel by its own norm; the first step knows them all and sets the panels
+// and their parts right.  Matrices of one panel take one launch in all, from the
+// norm to the update.  What bounds it are launches
 // and latency: the float32 matrix instructions take 16 times the half-precision
 // ones' time, and still only 2 us a step for 64 rows by 64 columns, and they
 // keep the full 24 bits where few rows average few roundings out.
@@ -208,7 +210,7 @@ __device__ __forceinline__ double load_panel(Narrow<NB, W>& l, const OrthoArgs& 
     return s;
 }
 
-// The panel times 1 / (|M| + eps).  (Values past the matrix stay zero, also
+// The panel times `inv`.  (Values past the matrix stay zero, also
 // where the norm is no number.)
 template <int NB, int W>
 __device__ __forceinline__ void scale_panel(Narrow<NB, W>& l, const OrthoArgs& a, int p0, int width, double inv)
@@ -217,6 +219,18 @@ __device__ __forceinline__ void scale_panel(Narrow<NB, W>& l, const OrthoArgs& a
     const int n = a.tall ? a.cols : a.rows, m = a.tall ? a.rows : a.cols;
     for (int i = threadIdx.x >> 6; i < n; i += kWaves)
         for (int c = threadIdx.x & 63; c < min(width, m - p0); c += 64) l.x[i * N::LD + c] = (float)(l.x[i * N::LD + c] * inv);
+}
+
+// The sum of the threads' `s`, by way of l.sums.
+template <int NB, int W>
+__device__ __forceinline__ double block_sum(Narrow<NB, W>& l, double s)
+{
+    for (int k = 32; k >= 1; k >>= 1) s += __shfl_xor(s, k);
+    if ((threadIdx.x & 63) == 0) l.sums[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = 0.0;
+    for (int k = 0; k < kWaves; ++k) s += l.sums[k];
+    return s;
 }
 
 template <int NB, int W>
@@ -259,12 +273,7 @@ __global__ __launch_bounds__(kThreads) void ortho_whole_kernel(OrthoArgs a, int 
 {
     __shared__ __align__(16) Narrow<NB, W> l;
     const int mat = blockIdx.x;
-    double s = load_panel(l, a, mat, 0, width);
-    for (int k = 32; k >= 1; k >>= 1) s += __shfl_xor(s, k);
-    if ((threadIdx.x & 63) == 0) l.sums[threadIdx.x >> 6] = s;
-    __syncthreads();
-    s = 0.0;
-    for (int k = 0; k < kWaves; ++k) s += l.sums[k];
+    const double s = block_sum(l, load_panel(l, a, mat, 0, width));
     scale_panel(l, a, 0, width, inverse_of(s, a.eps));
     for (int k = 0; k < steps; ++k) {
         __syncthreads();
@@ -301,11 +310,9 @@ __global__ __launch_bounds__(kThreads) void ortho_first_kernel(OrthoArgs a, Pane
 {
     __shared__ __align__(16) Narrow<NB, W> l;
     const int mat = blockIdx.x / p.panels, panel = blockIdx.x - mat * p.panels;
-    load_panel(l, a, mat, panel * p.width, p.width);
-    bool nothing;
-    const double inv = inverse_norm(a, mat, nothing);
-    __syncthreads();
-    scale_panel(l, a, panel * p.width, p.width, inv);
+    const double s = block_sum(l, load_panel(l, a, mat, panel * p.width, p.width));
+    if (threadIdx.x == 0) a.partial[(int64_t)mat * p.panels + panel] = s;
+    scale_panel(l, a, panel * p.width, p.width, s > 0.0 ? 1.0 / sqrt(s) : 0.0);
     __syncthreads();
     leave_panel(l, a, p, mat, panel, 0);
 }
@@ -326,19 +333,38 @@ __global__ __launch_bounds__(kThreads) void ortho_step_kernel(OrthoArgs a, Panel
     const floatx4* parts = reinterpret_cast<const floatx4*>(a.sums) + ((int64_t)p.from * a.batch + mat) * p.panels * N::TRI * 64;
     // a thread's vectors of A's blocks; eight parts' loads of all of them in flight
     constexpr int MINE = (N::TRI * 64 + kThreads - 1) / kThreads, AHEAD = 8;
-    floatx4 s[MINE] = {};
-    for (int z = 0; z < p.panels; z += AHEAD) {
-        floatx4 v[AHEAD][MINE];
+    floatx4 v[AHEAD][MINE], s[MINE] = {};
+    auto fetch = [&](int z) {
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
 #pragma unroll
             for (int i = 0; i < MINE; ++i)
                 v[k][i] = parts[(int64_t)min(z + k, p.panels - 1) * N::TRI * 64 + min((int)threadIdx.x + i * kThreads, N::TRI * 64 - 1)];
+    };
+    fetch(0);
+    // The panels' own norms beside the matrix's, a lane a panel: what X was left
+    // divided by too much, and the square of that for the parts of A.
+    float own = 1.f, square = 1.f;
+    if (p.first) {
+        const int z = threadIdx.x & 63;
+        const double mine = z < p.panels ? a.partial[(int64_t)mat * p.panels + z] : 0.0;
+        double all = mine;
+        for (int k = 32; k >= 1; k >>= 1) all += __shfl_xor(all, k);
+        const double f = sqrt(mine) * inverse_of(all, a.eps);
+        own = (float)f;
+        square = (float)(f * f);
+    }
+    auto of_panel = [](float v, int z) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), z)); };
+    for (int z = 0;; z += AHEAD) {
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
-            if (z + k < p.panels)
+            if (z + k < p.panels) {
+                const float w = of_panel(square, p.first ? z + k : 0);
 #pragma unroll
-                for (int i = 0; i < MINE; ++i) s[i] += v[k][i];
+                for (int i = 0; i < MINE; ++i) s[i] += w * v[k][i];
+            }
+        if (z + AHEAD >= p.panels) break;
+        fetch(z + AHEAD);
     }
 #pragma unroll
     for (int i = 0; i < MINE; ++i) {
@@ -348,6 +374,7 @@ __global__ __launch_bounds__(kThreads) void ortho_step_kernel(OrthoArgs a, Panel
         block_of(t / 64, bi, bj);
         put_block<N::LDA>(l.a, bi, bj, t % 64, s[i]);
     }
+    const float scale = of_panel(own, p.first ? panel : 0);
     for (int t0 = threadIdx.x; t0 < vectors; t0 += XV * kThreads) {
         if (t0 != (int)threadIdx.x)
 #pragma unroll
@@ -355,7 +382,7 @@ __global__ __launch_bounds__(kThreads) void ortho_step_kernel(OrthoArgs a, Panel
 #pragma unroll
         for (int h = 0; h < XV; ++h) {
             const int t = t0 + h * kThreads, i = t / (p.width / 4), c = t % (p.width / 4) * 4;
-            if (t < vectors) *reinterpret_cast<floatx4*>(l.x + i * N::LD + c) = ahead[h];
+            if (t < vectors) *reinterpret_cast<floatx4*>(l.x + i * N::LD + c) = scale * ahead[h];
         }
     }
     __syncthreads();
@@ -374,13 +401,12 @@ hipError_t launch(const OrthoArgs& a, const OrthoPlan& plan, int steps, hipStrea
         ortho_whole_kernel<NB, W><<<a.batch, kThreads, 0, s>>>(a, plan.width, steps);
         return hipGetLastError();
     }
-    hipError_t e = launch_ortho_norm(a, s);
-    if (e != hipSuccess) return e;
-    PanelArgs p{plan.width, plan.panels, 0, false};
+    PanelArgs p{plan.width, plan.panels, 0, false, false};
     ortho_first_kernel<NB, W><<<a.batch * plan.panels, kThreads, 0, s>>>(a, p);
-    e = hipGetLastError();
+    hipError_t e = hipGetLastError();
     for (int k = 0; k < steps && e == hipSuccess; ++k) {
         p.from = k & 1;
+        p.first = k == 0;
         p.last = k + 1 == steps;
         ortho_step_kernel<NB, W><<<a.batch * plan.panels, kThreads, 0, s>>>(a, p);
         e = hipGetLastError();
@@ -392,6 +418,7 @@ hipError_t launch(const OrthoArgs& a, const OrthoPlan& plan, int steps, hipStrea
 constexpr int widest(int rows) { return rows == 16 ? 2048 : rows == 32 ? 512 : 256; }
 constexpr int whole(int rows) { return rows == 16 ? 2048 : rows == 32 ? 512 : 128; }
 constexpr int kPanels = 24;
+static_assert(kPanels <= 64, "a lane for each");
 
 }  // namespace
 
@@ -410,10 +437,9 @@ bool ortho_narrow_plan(const cbw_ortho_desc* d, OrthoPlan* p)
     p->width = w;
     p->panels = (m + w - 1) / w;
     if (p->panels == 1) return true;
-    p->parts = (int)std::min<int64_t>(512, std::max<int64_t>(1, (int64_t)d->rows * d->cols / 8192));
     const size_t tri = (size_t)(rows / 16) * (rows / 16 + 1) / 2 * 1024;
     size_t at = 0;
-    p->partial = ortho_region(at, (size_t)d->batch * p->parts * sizeof(double));
+    p->partial = ortho_region(at, (size_t)d->batch * p->panels * sizeof(double));
     p->x = ortho_region(at, (size_t)d->batch * p->panels * rows * w * 4);
     p->sums = ortho_region(at, (size_t)d->batch * p->panels * tri * 2);
     p->ws_bytes = at;

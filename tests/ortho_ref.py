@@ -62,7 +62,7 @@ def check(got, m, coefficients, steps, eps, what):
     which alike singular values would be sqrt(0.14), and in the last two."""
     f32, n = got.dtype == torch.float32, min(m.shape)
     want, bound = steps_of(m, coefficients, steps, eps,
-                           [f32 or k + 2 >= steps or coefficients[0] ** (2 * k) > 0.14 * n for k in range(steps)])
+                           [f32 or k + 2 >= steps or coefficients[0] < 1 or coefficients[0] ** (2 * k) > 0.14 * n for k in range(steps)])
     g = got.detach().cpu().double()
     assert g.shape == want.shape and torch.isfinite(g).all(), what
     bound += (U32 if f32 else 2.0 ** -8) * float(want.norm()) + 1e-37

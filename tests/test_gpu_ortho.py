@@ -58,6 +58,15 @@ def test_steps(size, out):
     assert torch.equal(o, _run(m, out, dtype)), "the same call, the same bits"
 
 
+def test_slow_coefficients():
+    """A first coefficient below 1, with one large singular value: its steps are B X for the most part, and take both parts."""
+    m = _draw(1, 200, 300, 8)[0]
+    u, v = torch.linalg.qr(torch.randn((200, 1), generator=torch.Generator().manual_seed(3)))[0], torch.randn((1, 300), generator=torch.Generator().manual_seed(4))
+    m = 0.01 * m / m.norm() + u @ (v / v.norm())
+    for out in ("f32", "bf16"):
+        ref.check(_run(m[None], out, coefficients=(0.25, 1.0, -0.25))[0], m, (0.25, 1.0, -0.25), 5, 1e-7, out)
+
+
 def test_large():
     m = _draw(1, 700, 1600, 2)
     for out in ("f32", "bf16"):
@@ -66,16 +75,15 @@ def test_large():
 
 
 @pytest.mark.parametrize("out", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,cols", [(640, 900), (1100, 600)])
-def test_large_batch(rows, cols, out):
-    """Enough for tiles of 256, the last ones half empty; one matrix of zeros."""
-    batch = 44
+@pytest.mark.parametrize("batch,rows,cols", [(44, 640, 900), (44, 1100, 600), (70, 300, 300), (86, 260, 270)])
+def test_large_batch(batch, rows, cols, out):
+    """Enough for tiles of 256 on both sides of a whole turn, the last ones half empty; one matrix of zeros."""
     m = _draw(1, rows, cols, 7) * torch.linspace(0.5, 2.0, batch)[:, None, None]
     m[1::2] = m[1::2].flip(2)
     m[9] = 0.0
     o = _run(m, out)
     assert bool((o[9] == 0).all())
-    for i in (0, 1, 43):
+    for i in (0, 1, batch - 1):
         ref.check(o[i], m[i], QUINTIC, 5, 1e-7, "matrix %d" % i)
     # the others are the same matrices at other sizes, which the norm takes off but for eps and its rounding
     for i in range(2, batch):
