@@ -606,6 +606,25 @@ int64_t likely_tiles(const GatedArgs& a, int tile, int width)
     return busy * ((mean + tile - 1) / tile) * ((a.K + width - 1) / width);
 }
 
+// Which kernel: by the tiles that even lengths would give.
+//
+// Tiles pay where they fill most of the chip and the experts have rows for them
+// (us, forward | backward, tiles against streaming: 1280 rows, 1024 -> 2560, 400
+// | 200 tiles of 128: 25.8 | 21.2 against 45 | 30; 512 rows, 2048 -> 2048, 128 |
+// 64 tiles: 28.9 | 31.8 against 22.1 | 13.4; 16 experts of 32 rows, 2048 -> 2048:
+// 70.8 | 40.2 against 67.9 | 37.0, of 64 rows alike).  Which tiles, by turns: one
+// of 256 x 256 counts 1, of 192 rows 0.8, of 128 x 128, two to a CU, 0.77, and
+// 0.57 where it is half empty or more (3840 rows, 1024 -> 2560, forward, 300, 400
+// or 1200 tiles: 61.4, 49.8, 59.1; backward, 150, 200 or 600: 37.3, 34.5, 43.9;
+// 32 experts of 256 rows, 2048 -> 2048: 171, 216, 210 and 95, 120, 117).
+//
+// Streaming, 64 rows read the filters once where 16 read them several times, if
+// that leaves a workgroup for each CU (4 experts of 48 rows, 2048 -> 1024: 12.0 |
+// 12.7 with 64 rows, 12.7 | 9.4 with 16; 512 rows above: 22.1 | 13.4 and 34 | 21).
+//
+// float32, tiles of 64 and streaming: 32 experts of 50 rows, 512 -> 512, 512 | 256
+// tiles, 25.2 | 17.8 and 36.6 | 21.6; 8 experts of 100 rows, 256 | 128 tiles, 16.4
+// | 17.0 and 20.1 | 12.2; of 20 rows, 512 -> 1024, 15.3 | 16.3 and 12.3 | 9.4.
 template <typename T, bool BACK>
 hipError_t launch(const GatedArgs& a, hipStream_t s)
 {
@@ -613,18 +632,19 @@ hipError_t launch(const GatedArgs& a, hipStream_t s)
     constexpr int W = BACK ? 1 : 2;   // lines of the filters to a feature
     const int64_t mean = a.rows / std::max<int64_t>(1, std::min<int64_t>(a.E, a.rows));
     if constexpr (BF16) {
-        if (mean >= 160 && likely_tiles(a, 256, 256 / W) >= 200) {
-            // 192 rows take 0.8 of the time of 256, and where that fills the last turn
-            // of the workgroups better, less in all (4099 rows, 1024 -> 2816, 374 tiles
-            // or 484, us: 50.9 for 55.6; 16384 rows, 2048 -> 4096, turns alike: 582 for 551)
+        const int64_t small = likely_tiles(a, 128, 128 / W);
+        if (mean > 64 && small >= 200) {
             auto turns = [&](int rows) { return (likely_tiles(a, rows, 256 / W) + CBW_NUM_CUS - 1) / CBW_NUM_CUS; };
-            if (4 * turns(192) < 5 * turns(256)) return launch_tiles<T, BACK, 256, 192, 2, 4>(a, s);
+            const int64_t last = small % (2 * CBW_NUM_CUS);
+            const double by256 = (double)turns(256), by192 = 0.8 * (double)turns(192);
+            const double by128 = 0.77 * (double)(small / (2 * CBW_NUM_CUS)) + (last > CBW_NUM_CUS ? 0.77 : last > 0 ? 0.57 : 0.0);
+            if (by128 < std::min(by256, by192)) return launch_tiles<T, BACK, 128, 128, 2, 2>(a, s);
+            if (by192 < by256) return launch_tiles<T, BACK, 256, 192, 2, 4>(a, s);
             return launch_tiles<T, BACK, 256, 256, 2, 4>(a, s);
         }
-        if (mean > 16 && likely_tiles(a, 128, 128 / W) >= 200) return launch_tiles<T, BACK, 128, 128, 2, 2>(a, s);
-        if (mean > 64) return launch_stream<T, BACK, 64, 4, 4, 2>(a, s);
+        if (mean > 16 && likely_tiles(a, 64, 64 / W) >= CBW_NUM_CUS) return launch_stream<T, BACK, 64, 4, 4, 2>(a, s);
     } else {
-        if (mean > 16 && likely_tiles(a, 64, 64 / W) >= 400) return launch_tiles<T, BACK, 64, 64, 2, 2>(a, s);
+        if (mean > 32 && likely_tiles(a, 64, 64 / W) >= CBW_NUM_CUS) return launch_tiles<T, BACK, 64, 64, 2, 2>(a, s);
     }
     return launch_stream<T, BACK, 64, 1, 4, 2>(a, s);
 }

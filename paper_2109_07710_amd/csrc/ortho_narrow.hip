@@ -432,6 +432,11 @@ bool ortho_narrow_plan(const cbw_ortho_desc* d, OrthoPlan* p)
     if (w > whole(rows)) {
         if (width(kPanels) > widest(rows)) return false;
         w = std::max(width(kPanels), rows == 16 ? 256 : rows == 32 ? 128 : 64);
+        // Narrow panels are quicker, while there is a CU for each (64 x 576, one matrix
+        // and 16 of them, us: 48.5 and 58.7, by 128 columns 55.6 and 60.0); past that
+        // fewer are (22 x 63 x 773: 90.6 and 73.2; 32 x 24 x 3000 by 128, 512: 79, 68).
+        // Four of 16 rows find room on a CU (100 x 10 x 3000 by 256, 2048: 88, 95).
+        while (rows > 16 && (int64_t)d->batch * ((m + w - 1) / w) > CBW_NUM_CUS && 2 * w <= widest(rows)) w *= 2;
     }
     p->rows = rows;
     p->width = w;

@@ -88,6 +88,7 @@ LARGE = [
     (6, 5001, 72, 1032, "f32"),        # float32 tiles
     (100, 3000, 264, 264, "bf16"),     # more experts than lanes
     (100, 3000, 132, 264, "f32"),
+    (80, 4000, 132, 264, "f32"),
 ]
 
 
