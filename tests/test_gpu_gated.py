@@ -222,6 +222,28 @@ def test_captured_and_on_another_stream(dtype, rows):
             assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("E,K", [(1, 2064), (64, 72)])
+def test_rows_past_32_bits(E, K):
+    """Rows so far apart that their addresses pass 2^32 elements: bit for bit what adjacent ones give, large tiles and streaming."""
+    rows, C, far = 4400, 64, (1 << 20) - 8
+    off = _lengths(E, rows, 4) if E > 1 else [0, rows]
+    x, w, dy, w2, _ = (t.cuda() for t in _draw(off, rows, C, K, "bf16", 8))
+    o = _off(off)
+    near = cb.GatedDesc.make(E, rows, C, K)
+    H, GU, dGU = (_nan(rows, n * K, "bf16") for n in (1, 2, 2))
+    cb.expert_gated_fwd(near, x, w, o, H, GU)
+    cb.expert_gated_bwd(near, dy, w2, o, GU, dGU)
+    d = cb.GatedDesc.make(E, rows, C, K, x_stride=far, h_stride=far, gu_stride=far)
+    space = [torch.empty(rows * far, dtype=torch.bfloat16, device="cuda").view(rows, far) for _ in range(3)]
+    X, h, gu = space[0][:, :C], space[1][:, :K], space[2][:, :2 * K]
+    X.copy_(x)
+    cb.expert_gated_fwd(d, X, w, o, h, gu)
+    assert torch.equal(h, H) and torch.equal(gu, GU)
+    X.copy_(dy)
+    cb.expert_gated_bwd(d, X, w2, o, gu, gu)
+    assert torch.equal(gu, dGU)
+
+
 def test_offsets_without_sense_stay_inside():
     """Decreasing and out-of-range offsets: nothing outside the rows is written, and the call ends."""
     rows, C, K = 300, 64, 128

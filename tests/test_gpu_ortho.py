@@ -157,10 +157,12 @@ def test_sizes_of_values(size):
     ref.check(_run(m, eps=eps)[0], m[0], QUINTIC, 5, eps, "%g" % size)
 
 
-def test_captured():
+@pytest.mark.parametrize("first,second", [((2, 96, 200), (1, 300, 260)), ((3, 64, 576), (70, 260, 300)), ((9, 16, 40), (2, 2000, 30))],
+                         ids=["general", "panels_large", "whole_tall"])
+def test_captured(first, second):
     """In a graph with another call over its own workspace, replayed with other inputs between eager calls."""
-    da, db = cb.OrthoDesc.make(96, 200, 2), cb.OrthoDesc.make(300, 260, 1, "f32", "bf16")
-    sets = [(_draw(2, 96, 200, s).cuda(), _draw(1, 300, 260, s + 9).cuda()) for s in range(3)]
+    da, db = cb.OrthoDesc.make(*first[1:], first[0]), cb.OrthoDesc.make(*second[1:], second[0], "f32", "bf16")
+    sets = [(_draw(*first, s).cuda(), _draw(*second, s + 9).cuda()) for s in range(3)]
     a, b = (t.clone() for t in sets[0])
     oa, ob = torch.empty_like(a), torch.empty(b.shape, dtype=torch.bfloat16, device="cuda")
     wa, wb, we = _workspace(da), _workspace(db), torch.empty(max(_workspace(da).numel(), _workspace(db).numel()), dtype=torch.uint8, device="cuda")
@@ -185,6 +187,39 @@ def test_captured():
         step(ea, eb, we, we)
         torch.cuda.synchronize()
         assert torch.equal(oa, ea) and torch.equal(ob, eb)
+
+
+@pytest.mark.parametrize("rows,cols", [(3, 1 << 20), ((1 << 20) - 1, 2)])
+def test_longest(rows, cols):
+    m = _draw(1, rows, cols, 9)
+    co = QUINTIC if rows < cols else CUBIC
+    ref.check(_run(m, coefficients=co)[0], m[0], co, 5, 1e-7, "longest")
+
+
+def test_rows_past_32_bits():
+    """Rows so far apart that their addresses pass 2^32 elements, in M and in O."""
+    rows, cols, stride = 2100, 40, 1 << 21
+    m = _draw(1, rows, cols, 10)[0]
+    M = torch.empty(rows * stride, dtype=torch.bfloat16, device="cuda").view(rows, stride)[:, :cols]
+    O = torch.empty(rows * stride, dtype=torch.bfloat16, device="cuda").view(rows, stride)[:, :cols]
+    M.copy_(m.to(torch.bfloat16))
+    d = cb.OrthoDesc.make(rows, cols, 1, "bf16", "bf16", in_stride=stride, out_stride=stride)
+    cb.grad_orthogonalize(d, M, O, _workspace(d))
+    assert torch.equal(O, _run(m.to(torch.bfloat16).float()[None], "bf16", "bf16")[0])
+
+
+def test_two_streams_at_once():
+    """Calls of the same descriptor on two streams, each with its own workspace."""
+    m = [_draw(4, 260, 300, s).cuda() for s in (11, 12)]
+    d = cb.OrthoDesc.make(260, 300, 4)
+    want = [_run(x) for x in m]
+    streams, ws, out = [torch.cuda.Stream() for _ in m], [_workspace(d) for _ in m], [torch.zeros_like(x) for x in m]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, x, w, o in zip(streams, m, ws, out):
+            cb.grad_orthogonalize(d, x, o, w, stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(out, want))
 
 
 def test_update_of_an_expert_layer():
