@@ -768,43 +768,45 @@ __global__ __launch_bounds__(512) void ortho_large_kernel(OrthoArgs a, StepArgs 
 }
 
 // The parts of split tiles of 64 x 64, added in order, and what becomes of them.
+// A workgroup takes a quarter, what one wave left, so that the loads of most
+// splits are in flight at once (256 x 2304, ten tiles in twelve parts, a whole
+// call: 128.8 us for 139.3 with a workgroup a tile).
 template <int STAGE>
-__global__ __launch_bounds__(256) void ortho_sum_kernel(OrthoArgs a, StepArgs st)
+__global__ __launch_bounds__(128) void ortho_sum_kernel(OrthoArgs a, StepArgs st)
 {
-    constexpr int T = 64;
-    __shared__ __align__(1024) float lds[T * T];
+    constexpr int T = 64, S = T / 2, THREADS = 128;
+    __shared__ __align__(1024) float lds[S * S];
     const Tiles tiles = tiles_of<STAGE, T>(a);
-    const int tile = blockIdx.x;
+    const int tile = blockIdx.x / 4, quarter = blockIdx.x % 4;
     if (tile >= tiles.count) return;
     const Spot s = spot_of<STAGE, T>(a, tiles, tile);
     if (!tiles.listed && a.nothing[s.mat] != 0) return;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    // fragment (i, j) of this wave's 32 x 32
-    auto at = [&](int i, int j) { return wave * 256 + (i * 2 + j) * 64 + lane; };
+    const Spot part{s.mat, s.i0 + quarter % 2 * S, s.j0 + quarter / 2 * S};
     const int nothing = a.nothing[0];
-    Meets<STAGE, T, 256> meets;
-    meets.load(a, st, s);
-    const floatx4* sums = reinterpret_cast<const floatx4*>(a.sums) + (int64_t)tile * st.split * (T * T / 4);
-    floatx4 acc[2][2] = {};
-    constexpr int AHEAD = 4;   // parts whose loads are in flight
+    Meets<STAGE, S, THREADS> meets;
+    meets.load(a, st, part);
+    const floatx4* sums = reinterpret_cast<const floatx4*>(a.sums) + (int64_t)tile * st.split * (T * T / 4) + quarter * (S * S / 4) + threadIdx.x;
+    floatx4 acc[2] = {};
+    constexpr int AHEAD = 12;   // parts whose loads are in flight
     for (int z = 0; z < st.split; z += AHEAD) {
-        floatx4 v[AHEAD][2][2];
+        floatx4 v[AHEAD][2];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) v[k][i][j] = sums[(int64_t)min(z + k, st.split - 1) * (T * T / 4) + at(i, j)];
+            for (int h = 0; h < 2; ++h) v[k][h] = sums[(int64_t)min(z + k, st.split - 1) * (T * T / 4) + h * THREADS];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
             if (z + k < st.split)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[i][j] += v[k][i][j];
+                for (int h = 0; h < 2; ++h) acc[h] += v[k][h];
     }
     if (a.batch == 1 && nothing) return;
-    finish_tile<STAGE, T, 2, 2>(a, st, s, acc, meets, lds);
+    // vector n is lane n % 64's of fragment (n / 128, n / 64 % 2)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<floatx4*>(Square<S>::chunk(lds, (threadIdx.x >> 6) * 16 + (threadIdx.x & 15), h * 4 + (threadIdx.x >> 4 & 3))) = acc[h];
+    __syncthreads();
+    finish<STAGE, S, THREADS>(a, st, part, STAGE != UPDATE && s.i0 != s.j0, meets, lds);
 }
 
 template <int STAGE, bool PAIR, int T, int NWP, int NWQ, int SUB>
@@ -814,7 +816,7 @@ hipError_t launch_tiles(const OrthoArgs& a, StepArgs st, const OrthoDeal& d, hip
     ortho_product_kernel<STAGE, PAIR, T, NWP, NWQ, SUB><<<d.tiles * d.split, NWP * NWQ * 64, 0, s>>>(a, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || d.split == 1) return e;
-    if constexpr (T == 64) ortho_sum_kernel<STAGE><<<d.tiles, 256, 0, s>>>(a, st);
+    if constexpr (T == 64) ortho_sum_kernel<STAGE><<<4 * d.tiles, 128, 0, s>>>(a, st);
     return hipGetLastError();
 }
 
@@ -858,8 +860,10 @@ int64_t round_up(int64_t v, int64_t by) { return (v + by - 1) / by * by; }
 
 // How a product of `tiles(side)` tiles of `len` reduction indices is dealt out.
 // Tiles of 64 take some 0.5 us a step beside 4.4 for the start and the end; the
-// parts of a split one 2 beside their steps, and the launch that adds them up
-// 3.5 and 0.25 a part (us, 3 x 333 x 1001 and 256 x 2304, measured by launches).
+// parts of a split one and the launch that adds them up 7.5 beside their steps,
+// and 0.25 a part.  (With 5.5 there more tiles were split, and calls took, us: 400 x
+// 2000 198 for 164, 6 x 300 x 700 199 for 173, 3 x 333 x 1001 175 for 166; with
+// 4.5, 256 x 2304 166 for 128; with 9.5 as with 7.5.)
 template <typename F>
 OrthoDeal deal(F tiles, int64_t len, bool pair, bool by128, bool by256)
 {
@@ -871,7 +875,7 @@ OrthoDeal deal(F tiles, int64_t len, bool pair, bool by128, bool by256)
     const int64_t steps = len / (pair ? 32 : 64);
     double best = 4.4 + 0.5 * (double)steps - 1.0;   // (no split for less than 1 us)
     for (int s = 2; d.side == 64 && s <= steps && s <= 24 && (int64_t)d.tiles * s <= 2 * CBW_NUM_CUS; ++s) {
-        const double us = 5.5 + 0.25 * s + 0.5 * (double)((steps + s - 1) / s);
+        const double us = 7.5 + 0.25 * s + 0.5 * (double)((steps + s - 1) / s);
         if (us < best) {
             best = us;
             d.split = s;
