@@ -315,8 +315,8 @@ struct Tiles {
 // What bounds it: a step of a 256 x 256 tile takes 1.5 us, 1.07 of them matrix
 // instructions at the clock that they leave, and a tile some 10 us beyond its
 // steps; its results are ready at once in every CU (16384 rows, 2048 -> 4096, eight
-// uneven experts: forward 539 us, 1020 TFLOP/s, nine turns of tiles for the work
-// of 8.5; backward 369, 740 TFLOP/s and 870 MB in and out).  Four waves with 128
+// uneven experts: forward 524 us, 1050 TFLOP/s, nine turns of tiles for the work
+// of 8.5; backward 366, 750 TFLOP/s and 870 MB in and out).  Four waves with 128
 // x 128 sums each would halve the LDS reads but spill (920 us for 535); letting
 // the stores run on into the next tile's steps cost registers too (568 for 554).
 template <typename T, bool BACK, int TP, int TQ, int NWP, int NWQ>
