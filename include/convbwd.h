@@ -564,8 +564,9 @@ int grad_clip(const cbw_grad* grads, int32_t n, int32_t kind, float max_norm, fl
  * (or, the same, with A = X^T X from the right where it has more rows than
  * columns).  A matrix of zeros gives zeros, one with a NaN or an infinity NaN
  * throughout.  X is held in float32 and the products take 22 bits of each
- * value; with a bf16 result, 11 in the first steps, while singular values that
- * are all alike would still be below 0.37. */
+ * value; with a bf16 result and a of at least 1, 11 in the first steps, while
+ * singular values that are all alike would still be below 0.37.  Calls that
+ * overlap, captured ones among them, need a workspace each. */
 typedef struct {
     int32_t rows, cols, batch;          /* batch 0 is allowed                    */
     int32_t dtype;                      /* cbw_dtype of M                        */

@@ -196,6 +196,19 @@ def test_longest(rows, cols):
     ref.check(_run(m, coefficients=co)[0], m[0], co, 5, 1e-7, "longest")
 
 
+def test_one_large_matrix():
+    """5120 x 5120, ten times the same block on its diagonal: every block as alone beside a norm sqrt(10) as large, the rest zero."""
+    n, blocks = 512, 10
+    m = _draw(1, n, n, 13)[0]
+    M = torch.block_diag(*[m] * blocks)
+    o = _run(M[None])[0]
+    eps = (blocks ** 0.5 - 1.0) * float(m.double().norm())
+    for i in range(blocks):
+        ref.check(o[i * n:(i + 1) * n, i * n:(i + 1) * n], m, QUINTIC, 5, eps, "block %d" % i)
+        o[i * n:(i + 1) * n, i * n:(i + 1) * n] = 0.0
+    assert not bool(o.any())
+
+
 def test_rows_past_32_bits():
     """Rows so far apart that their addresses pass 2^32 elements, in M and in O."""
     rows, cols, stride = 2100, 40, 1 << 21
