@@ -563,10 +563,12 @@ int grad_clip(const cbw_grad* grads, int32_t n, int32_t kind, float max_norm, fl
  *
  * (or, the same, with A = X^T X from the right where it has more rows than
  * columns).  A matrix of zeros gives zeros, one with a NaN or an infinity NaN
- * throughout.  X is held in float32 and the products take 22 bits of each
- * value; with a bf16 result and a of at least 1, 11 in the first steps, while
- * singular values that are all alike would still be below 0.37.  Calls that
- * overlap, captured ones among them, need a workspace each. */
+ * throughout.  X is held in float32.  The products take 22 bits of each value
+ * (of tiny ones fewer: to within 2^-36 of X's and 2^-35 of A's and B's), those of
+ * matrices with at most 64 rows or columns 24, unless these are very long.  The
+ * type of O changes nothing but its rounding: a bf16 result is the float32 one,
+ * rounded once.  Calls that overlap, captured ones among them, need a workspace
+ * each. */
 typedef struct {
     int32_t rows, cols, batch;          /* batch 0 is allowed                    */
     int32_t dtype;                      /* cbw_dtype of M                        */

@@ -172,9 +172,8 @@ struct OrthoDeal {
 // zeros to multiples of 64 or 128.
 struct OrthoPlan {
     int np, mp;
-    int coarse;                             // steps on high parts alone, the first ones
     int parts;                              // partial sums of a matrix's norm
-    OrthoDeal deal[2][3];                   // on high parts and on pairs: of A, A A and B X
+    OrthoDeal deal[3];                      // of A, A A and B X
     int rows, width, panels;                // up to 64 rows: X in panels of columns; rows 0: as above
     size_t partial, nothing, x, planes[2], gram, poly, sums, ws_bytes;   // byte offsets
 };
@@ -208,7 +207,7 @@ struct OrthoArgs {
 struct StepArgs {
     int from;                   // which of the planes holds X
     int split;                  // workgroups that share a tile's reduction
-    bool last, pair, next_pair;
+    bool last;
     bool quarters;              // those of the 256 x 256 tiles that do not fill a turn
 };
 struct PanelArgs {

@@ -12,14 +12,12 @@
 // near to 64 bits as the same steps in float32 (2.1e-6 against 2.1e-6 of the
 // result's 2-norm, 256 x 2304 of full rank), at three instructions of the
 // half-precision rate, which is a fifth of the float32 instructions' time.
-// Where the update is stored in bf16, the first steps take the high parts
-// alone: what they leave off, 2^-11 of B X but nothing of the a X beside it,
-// counts for little while the singular values are small.  With all of them
-// alike, the worst case, they are a^k / sqrt(n) after k steps; while that is
-// below sqrt(0.14) and two more steps follow, the update's error stays below
-// 4e-4 of its 2-norm, against the 1.7e-3 of its rounding (n = 1024, full rank:
-// 3.5e-4, flat: 3.6e-5; n = 256: 5e-5).  A step too many costs 8e-4 at n = 256
-// and 3e-3 at 64.
+// Every step takes both parts, whatever the type of the result.  High parts alone
+// in the first steps would do for matrices whose singular values are alike, and
+// for those only: with four live rows of 1024, three of five such steps leave an
+// error of 5e-3 to 9e-3 of the 2-norm, where rounding the result to bf16 leaves
+// 1.7e-3, and one live row loses as much in its first step alone, so that no
+// number of such steps follows from the sizes.
 #include "common.hpp"
 #include "block_kernels.hpp"
 #include "expert_tiles.hpp"
@@ -130,34 +128,32 @@ __device__ __forceinline__ double inverse_norm(const OrthoArgs& a, int mat, bool
     return inverse_of(s, a.eps);
 }
 
-// Where a matrix's planes of `ld` columns and `rows` rows (of one matrix) hold
-// the high part of (i, j), and how much further its low part lies.  Products
-// on pairs find 32 high parts and the same columns' 32 low parts in each 128
-// bytes, so that a step of the reduction is whole lines; those on high parts
-// alone find them in a plane of their own.
+// Where a matrix's planes of `ld` columns hold the high part of (i, j); its low
+// part lies kLow further.  32 high parts and the same columns' 32 low parts share
+// 128 bytes, so that a step of a product's reduction is whole lines.
+constexpr int kLow = 32;
 struct Plane {
-    int64_t mat, low;
+    int64_t mat;
     int ld;
-    bool pair;
-    __device__ Plane(bool pr, int which, int batch, int rows, int columns)
-        : mat((int64_t)which * rows * columns * (pr ? 2 : 1)), low(pr ? 32 : (int64_t)batch * rows * columns), ld(columns), pair(pr) {}
-    __device__ __forceinline__ int64_t at(int i, int j) const
-    {
-        return mat + (pair ? (int64_t)i * ld * 2 + (j >> 5) * 64 + (j & 31) : (int64_t)i * ld + j);
-    }
+    __device__ Plane(int which, int rows, int columns) : mat((int64_t)which * rows * columns * 2), ld(columns) {}
+    __device__ __forceinline__ int64_t at(int i, int j) const { return mat + (int64_t)i * ld * 2 + (j >> 5) * 64 + (j & 31); }
 };
-__device__ __forceinline__ void put_x(const OrthoArgs& a, const Plane& plane, _Float16* to, int i, int j, const float (&x)[8])
+__device__ __forceinline__ void put_pair(_Float16* at, const float (&v)[8])
+{
+    const Pair w = split(v);
+    *reinterpret_cast<uint4*>(at) = w.hi;
+    *reinterpret_cast<uint4*>(at + kLow) = w.lo;
+}
+__device__ __forceinline__ void put_x(const Plane& plane, _Float16* to, int i, int j, const float (&x)[8])
 {
     float v[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = x[k] * kX;
-    const Pair w = split(v);
-    *reinterpret_cast<uint4*>(to + plane.at(i, j)) = w.hi;
-    if (plane.pair) *reinterpret_cast<uint4*>(to + plane.at(i, j) + plane.low) = w.lo;
+    put_pair(to + plane.at(i, j), v);
 }
 
 // X and its planes, 64 x 64 values a workgroup, zeros past the matrix.
-__global__ __launch_bounds__(256) void ortho_start_kernel(OrthoArgs a, bool pair)
+__global__ __launch_bounds__(256) void ortho_start_kernel(OrthoArgs a)
 {
     __shared__ float tile[64][65];
     const int bx = a.mp / 64, by = a.np / 64;
@@ -192,7 +188,7 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(OrthoArgs a, bool pair
         }
         return;
     }
-    const Plane plane(pair, mat, a.batch, a.np, a.mp);
+    const Plane plane(mat, a.np, a.mp);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int t = threadIdx.x + h * 256, r = t / 8, c = t % 8 * 8;
@@ -213,7 +209,7 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(OrthoArgs a, bool pair
         float* x = a.x + (int64_t)mat * a.np * a.mp + (int64_t)(i0 + i) * a.mp + j0 + j;
         *reinterpret_cast<float4*>(x) = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
         *reinterpret_cast<float4*>(x + 4) = make_float4(v[h][4], v[h][5], v[h][6], v[h][7]);
-        put_x(a, plane, a.planes[0], i0 + i, j0 + j, v[h]);
+        put_x(plane, a.planes[0], i0 + i, j0 + j, v[h]);
     }
 }
 
@@ -329,10 +325,10 @@ template <int STAGE, int T, int THREADS>
 struct Meets {
     static constexpr int VECS = STAGE == GRAM ? 1 : T * T / 8 / THREADS;
     uint4 v[VECS][2];
-    __device__ __forceinline__ void load(const OrthoArgs& a, const StepArgs& st, const Spot& s)
+    __device__ __forceinline__ void load(const OrthoArgs& a, const Spot& s)
     {
         if (STAGE == GRAM) return;
-        const Plane square(st.pair, s.mat, a.batch, a.np, a.np);
+        const Plane square(s.mat, a.np, a.np);
         const int thread = my_thread();
 #pragma unroll
         for (int k = 0; k < VECS; ++k) {
@@ -344,7 +340,7 @@ struct Meets {
             } else {
                 const _Float16* g = a.gram + square.at(s.i0 + q, s.j0 + p);
                 v[k][0] = *reinterpret_cast<const uint4*>(g);
-                v[k][1] = *reinterpret_cast<const uint4*>(g + square.low);
+                v[k][1] = *reinterpret_cast<const uint4*>(g + kLow);
             }
         }
     }
@@ -359,13 +355,8 @@ __device__ __forceinline__ void finish(const OrthoArgs& a, const StepArgs& st, c
     using Sq = Square<T>;
     const bool turned = STAGE == UPDATE && st.last && a.tall;
     _Float16* out = STAGE == GRAM ? a.gram : a.poly;
-    const Plane square(st.pair, s.mat, a.batch, a.np, a.np), next(st.next_pair, s.mat, a.batch, a.np, a.mp);
-    auto put = [&](int i, int j, const float (&v)[8]) {
-        const Pair w = split(v);
-        const int64_t at = square.at(i, j);
-        *reinterpret_cast<uint4*>(out + at) = w.hi;
-        if (STAGE == GRAM || st.pair) *reinterpret_cast<uint4*>(out + at + square.low) = w.lo;
-    };
+    const Plane square(s.mat, a.np, a.np), wide(s.mat, a.np, a.mp);
+    auto put = [&](int i, int j, const float (&v)[8]) { put_pair(out + square.at(i, j), v); };
     const int thread = my_thread();
 #pragma unroll
     for (int u = 0; u < T * T / 8 / THREADS; ++u) {
@@ -386,7 +377,7 @@ __device__ __forceinline__ void finish(const OrthoArgs& a, const StepArgs& st, c
             if (!st.last) {
                 *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
                 *reinterpret_cast<float4*>(at + 4) = make_float4(v[4], v[5], v[6], v[7]);
-                put_x(a, next, a.planes[st.from ^ 1], s.i0 + q, s.j0 + p, v);
+                put_x(wide, a.planes[st.from ^ 1], s.i0 + q, s.j0 + p, v);
             } else if (!a.tall) {
                 store_out(a, s.mat, s.i0 + q, s.j0 + p, v);
             }
@@ -460,36 +451,35 @@ struct PairsAcross {
 };
 
 // A tile's operands, as they come into LDS: from step `first` on.  A step is 128
-// bytes of reduction indices of both: 64 high parts, or 32 pairs.
-template <int STAGE, bool PAIR, int T, int NW>
+// bytes of both: 32 reduction indices.
+constexpr int kStep = 32;
+template <int STAGE, int T, int NW>
 struct Feed {
-    static constexpr int KS = PAIR ? 32 : 64;                   // reduction indices of a step
-    using OP = Operand<uint16_t, T, STAGE == UPDATE, NW>;
-    using OQ = Operand<uint16_t, T, false, NW>;
+    using Along = Operand<uint16_t, T, false, NW>;
+    using OP = Operand<uint16_t, T, STAGE == UPDATE, NW>;   // (across: as its fragments are read)
+    using OQ = Along;
     static constexpr int COPIES = OP::COPIES + OQ::COPIES, TILE = OP::BYTES, STEP = 2 * TILE;
-    OP op;
+    std::conditional_t<STAGE == UPDATE, PairsAcross<T, NW>, Along> op;
     OQ oq;
-    PairsAcross<T, NW> across;
     const _Float16 *pb, *qb;
     int64_t pld, qld;
     int first, vp, vq;   // columns and rows there are
 
     __device__ __forceinline__ Feed(const OrthoArgs& a, const StepArgs& st, const Spot& s, int wave, int at) : first(at)
     {
-        pld = (STAGE == SQUARE ? a.np : a.mp) * (PAIR ? 2 : 1);
-        qld = (STAGE == GRAM ? a.mp : a.np) * (PAIR ? 2 : 1);
+        pld = (STAGE == SQUARE ? a.np : a.mp) * 2;
+        qld = (STAGE == GRAM ? a.mp : a.np) * 2;
         vq = min(T, a.np - s.i0);
         vp = min(T, (STAGE == UPDATE ? a.mp : a.np) - s.j0);
-        const Plane xs(PAIR, s.mat, a.batch, a.np, a.mp), gs(PAIR, s.mat, a.batch, a.np, a.np);
+        const Plane xs(s.mat, a.np, a.mp), gs(s.mat, a.np, a.np);
         const _Float16* x = a.planes[st.from];
         pb = STAGE == GRAM ? x + xs.at(s.j0, 0) : STAGE == SQUARE ? a.gram + gs.at(s.j0, 0) : x + xs.at(0, s.j0);
         qb = STAGE == GRAM ? x + xs.at(s.i0, 0) : STAGE == SQUARE ? a.gram + gs.at(s.i0, 0) : a.poly + gs.at(s.i0, 0);
         pb = uniform(pb);
         qb = uniform(qb);
         oq.init(wave, 0, qld);
-        if (STAGE != UPDATE) op.init(wave, 0, pld);
-        else if (PAIR) across.init(wave, vp, a.mp);
-        else op.init(wave, vp, pld);
+        if constexpr (STAGE == UPDATE) op.init(wave, vp, a.mp);
+        else op.init(wave, 0, pld);
     }
     static __device__ __forceinline__ const _Float16* uniform(const _Float16* p)
     {
@@ -513,13 +503,10 @@ struct Feed {
     __device__ __forceinline__ void copy(int wave, int step, char* to) const
     {
         const int64_t k = first + step;
-        if (STAGE == UPDATE) {
-            const u32x4_t r = make_rsrc_words(pb + k * KS * pld, (uint32_t)(((KS - 1) * pld + vp * (PAIR ? 2 : 1)) * 2));
-            if (PAIR) across.copy(wave, r, to);
-            else op.copy(wave, r, 0, 0, to);
-        } else {
+        if constexpr (STAGE == UPDATE)
+            op.copy(wave, make_rsrc_words(pb + k * kStep * pld, (uint32_t)(((kStep - 1) * pld + vp * 2) * 2)), to);
+        else
             op.copy(wave, make_rsrc_words(pb + k * 64, (uint32_t)(((vp - 1) * pld + 64) * 2)), 0, 64, to);
-        }
         oq.copy(wave, make_rsrc_words(qb + k * 64, (uint32_t)(((vq - 1) * qld + 64) * 2)), 0, 64, to + TILE);
     }
 };
@@ -530,28 +517,26 @@ struct Feed {
 // The steps of a tile are shared out to st.split workgroups, whose sums go to
 // memory where there are several; a launch of their own adds them up.
 //
-// What bounds them: tiles of 128 on pairs run at 1030 to 1070 TFLOP/s of fp16
-// products where they fill the chip (7 matrices 4096 x 2048: A 358 us, A A 191, B
-// X 675), a library product at 1200 to 1260; on high parts alone B X moves as
-// much of X for a third of the products (335 us, 137 of them X's way in and out).
-// One matrix of 2048 x 2048 has 136 tiles for 256 CUs (A 41 us).  Tiles of 64
-// wait: 0.5 us a step for 0.1 of matrix instructions, and 4 to 5 a launch.
-// (Counting them in and leaving that to the last workgroup of a tile took a
-// fence for the whole device in each, and 98 us in place of 28 for A of 2048 x
-// 2048 values, 136 tiles in 256 ranges.)
-template <int STAGE, bool PAIR, int T, int NWP, int NWQ, int SUB>
+// What bounds them: tiles of 128 run at 1030 to 1070 TFLOP/s of fp16 products
+// where they fill the chip (7 matrices 4096 x 2048: A 358 us, A A 191, B X 675), a
+// library product at 1200 to 1260.  One matrix of 2048 x 2048 has 136 tiles for
+// 256 CUs (A 41 us).  Tiles of 64 wait: 0.5 us a step for 0.1 of matrix
+// instructions, and 4 to 5 a launch.  (Counting them in and leaving that to the
+// last workgroup of a tile took a fence for the whole device in each, and 98 us
+// in place of 28 for A of 2048 x 2048 values, 136 tiles in 256 ranges.)
+template <int STAGE, int T, int NWP, int NWQ, int SUB>
 __global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs a, StepArgs st)
 {
     constexpr int NW = NWP * NWQ, FM = T / NWP / 16, FN = T / NWQ / 16;
-    using Fd = Feed<STAGE, PAIR, T, NW>;
+    using Fd = Feed<STAGE, T, NW>;
     using OP = typename Fd::OP;
     using OQ = typename Fd::OQ;
-    constexpr int KS = Fd::KS, COPIES = Fd::COPIES, TILE = Fd::TILE, STEP = Fd::STEP;
+    constexpr int COPIES = Fd::COPIES, TILE = Fd::TILE, STEP = Fd::STEP;
     constexpr int RING = 2 * SUB;
     __shared__ __align__(1024) char lds[RING * STEP > T * T * 4 ? RING * STEP : T * T * 4];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave / NWQ, wq = wave % NWQ;
-    const int len = (STAGE == GRAM ? a.mp : a.np) / KS;         // steps of a tile
+    const int len = (STAGE == GRAM ? a.mp : a.np) / kStep;         // steps of a tile
     const bool quarters = STAGE != UPDATE && T == 128 && st.quarters;
     const Tiles tiles = quarters ? tiles_of<STAGE, 256>(a) : tiles_of<STAGE, T>(a);
     const int taken = quarters ? large_tiles(tiles.count) : 0;
@@ -572,7 +557,7 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs 
 
     const int nothing = a.nothing[0];
     Meets<STAGE, T, NW * 64> meets;
-    if (T == 64 && st.split == 1) meets.load(a, st, s);
+    if (T == 64 && st.split == 1) meets.load(a, s);
     const Fd feed(a, st, s, wave, first);
     auto copy = [&](int step) { feed.copy(wave, step, lds + step % RING * STEP); };
 
@@ -587,7 +572,7 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs 
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = mfma_half(acc[i][j], p[i], q[j]);
     };
-    // A step's fragments: its halves, or its high and low parts.
+    // A step's fragments: its high and low parts.
     struct Fragments {
         uint4 p[2][FM], q[2][FN];
     };
@@ -601,10 +586,10 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs 
     };
     auto product = [&](const Fragments& f) {
         multiply(f.p[0], f.q[0]);
-        multiply(f.p[PAIR ? 0 : 1], f.q[1]);
-        if (PAIR) multiply(f.p[1], f.q[0]);
+        multiply(f.p[0], f.q[1]);
+        multiply(f.p[1], f.q[0]);
         // one or two reads between every few matrix instructions
-        constexpr int READS = 2 * (FM * (STAGE == UPDATE ? 2 : 1) + FN), MUL = FM * FN * (PAIR ? 3 : 2);
+        constexpr int READS = 2 * (FM * (STAGE == UPDATE ? 2 : 1) + FN), MUL = FM * FN * 3;
 #pragma unroll
         for (int i = 0; i < READS; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                    // an LDS read
@@ -652,7 +637,7 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs 
     } else {
         if (a.batch == 1 && nothing) return;
         // (tiles of 64 have the registers to ask for it at the start)
-        if (T > 64) meets.load(a, st, s);
+        if (T > 64) meets.load(a, s);
         finish_tile<STAGE, T, NWP, NWQ>(a, st, s, acc, meets, reinterpret_cast<float*>(lds));
     }
 }
@@ -661,28 +646,25 @@ __global__ __launch_bounds__(NWP* NWQ * 64) void ortho_product_kernel(OrthoArgs 
 // step.  A wave's 64 x 128 sums leave registers for two sets of fragments,
 // which take turns:
 //
-//   pairs        hi hi (meanwhile the low parts are read), lo hi, and behind the
-//                barrier hi lo (and the next step's high parts, into the sets
-//                that are free: those of the columns change places each step)
-//   high parts   the halves of a step, the barrier between them
+//   hi hi (meanwhile the low parts are read), lo hi, and behind the barrier hi lo
+//   (and the next step's high parts, into the sets that are free: those of the
+//   columns change places each step)
 //
-// (7 of 8 matrices 4096 x 2048, us, tiles of 128 and of 256: A on pairs 358 and
-// 284, on high parts 162 and 121, A A 191 and 160, 90 and 74.  B X gained
-// nothing, 344 and 353 on high parts, 686 and 682 on pairs: half of its time
-// goes into reading and writing X.)
-template <int STAGE, bool PAIR>
+// (7 of 8 matrices 4096 x 2048, us, tiles of 128 and of 256: A 358 and 284, A A
+// 191 and 160.  B X gained nothing, 686 and 682.)
+template <int STAGE>
 __global__ __launch_bounds__(512) void ortho_large_kernel(OrthoArgs a, StepArgs st)
 {
     static_assert(STAGE != UPDATE, "see above");
     constexpr int T = 256, NWQ = 4, FM = 8, FN = 4;
-    using Fd = Feed<STAGE, PAIR, T, 8>;
+    using Fd = Feed<STAGE, T, 8>;
     using OP = typename Fd::OP;
     using OQ = typename Fd::OQ;
     __shared__ __align__(1024) char lds[2 * Fd::STEP];
     static_assert(sizeof(lds) >= 128 * 128 * 4, "a quarter of a finished tile");
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave / NWQ, wq = wave % NWQ;
-    const int steps = (STAGE == GRAM ? a.mp : a.np) / Fd::KS;   // an even number: sizes are multiples of 128
+    const int steps = (STAGE == GRAM ? a.mp : a.np) / kStep;   // an even number: sizes are multiples of 128
     const Tiles tiles = tiles_of<STAGE, T>(a);
     const int count = large_tiles(tiles.count);
     if ((int)blockIdx.x >= count) return;
@@ -725,21 +707,19 @@ __global__ __launch_bounds__(512) void ortho_large_kernel(OrthoArgs a, StepArgs 
     for (int k0 = 0; k0 < steps; k0 += 2) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int k = k0 + u, hi = PAIR ? u : 0;
+            const int k = k0 + u, hi = u;
             read(u, 1, hi ^ 1, 1);
             multiply(hi, 0);
             interleave();
-            if (PAIR) {
-                multiply(hi ^ 1, 0);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            multiply(hi ^ 1, 0);
+            __builtin_amdgcn_sched_barrier(0);
             const Fd next = feed.here();
             wait_copies<0>();
             wait_reads();
             barrier();
             if (k + 2 < steps) copy(next, k + 2);
-            read(u ^ 1, 0, PAIR ? hi ^ 1 : 0, 0);   // (after the last step: what was there, unused)
-            multiply(PAIR ? hi : 1, 1);
+            read(u ^ 1, 0, hi ^ 1, 0);   // (after the last step: what was there, unused)
+            multiply(hi, 1);
             interleave();
             __builtin_amdgcn_sched_barrier(0);   // (the next reads have no registers yet)
         }
@@ -752,7 +732,7 @@ __global__ __launch_bounds__(512) void ortho_large_kernel(OrthoArgs a, StepArgs 
         const Spot part{s.mat, s.i0 + hq * 128, s.j0 + hp * 128};
         if (part.i0 >= a.np || part.j0 > part.i0) continue;   // (past the matrix; the mirrored quarter's)
         Meets<STAGE, 128, 512> meets;
-        meets.load(a, st, part);
+        meets.load(a, part);
         __syncthreads();   // every wave is done with the operands, or the quarter before
         if (wp == hp && wq >> 1 == hq) {
             const int lane = my_thread() & 63;
@@ -784,7 +764,7 @@ __global__ __launch_bounds__(128) void ortho_sum_kernel(OrthoArgs a, StepArgs st
     const Spot part{s.mat, s.i0 + quarter % 2 * S, s.j0 + quarter / 2 * S};
     const int nothing = a.nothing[0];
     Meets<STAGE, S, THREADS> meets;
-    meets.load(a, st, part);
+    meets.load(a, part);
     const floatx4* sums = reinterpret_cast<const floatx4*>(a.sums) + (int64_t)tile * st.split * (T * T / 4) + quarter * (S * S / 4) + threadIdx.x;
     floatx4 acc[2] = {};
     constexpr int AHEAD = 12;   // parts whose loads are in flight
@@ -809,51 +789,41 @@ __global__ __launch_bounds__(128) void ortho_sum_kernel(OrthoArgs a, StepArgs st
     finish<STAGE, S, THREADS>(a, st, part, STAGE != UPDATE && s.i0 != s.j0, meets, lds);
 }
 
-template <int STAGE, bool PAIR, int T, int NWP, int NWQ, int SUB>
+template <int STAGE, int T, int NWP, int NWQ, int SUB>
 hipError_t launch_tiles(const OrthoArgs& a, StepArgs st, const OrthoDeal& d, hipStream_t s)
 {
     st.split = d.split;
-    ortho_product_kernel<STAGE, PAIR, T, NWP, NWQ, SUB><<<d.tiles * d.split, NWP * NWQ * 64, 0, s>>>(a, st);
+    ortho_product_kernel<STAGE, T, NWP, NWQ, SUB><<<d.tiles * d.split, NWP * NWQ * 64, 0, s>>>(a, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || d.split == 1) return e;
     if constexpr (T == 64) ortho_sum_kernel<STAGE><<<4 * d.tiles, 128, 0, s>>>(a, st);
     return hipGetLastError();
 }
 
-template <int STAGE, bool PAIR>
+template <int STAGE>
 hipError_t launch_product(const OrthoArgs& a, const StepArgs& st, const OrthoDeal& d, hipStream_t s)
 {
     switch (d.side) {
     case 256:
         if constexpr (STAGE != UPDATE) {
             // (how many there are without the matrices of zeros, the kernels find)
-            ortho_large_kernel<STAGE, PAIR><<<d.tiles, 512, 0, s>>>(a, st);
+            ortho_large_kernel<STAGE><<<d.tiles, 512, 0, s>>>(a, st);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
             StepArgs rest = st;
             rest.quarters = true;
-            return launch_tiles<STAGE, PAIR, 128, 2, 2, 1>(a, rest, {128, 4 * std::min(d.tiles, kLeft), 1}, s);
+            return launch_tiles<STAGE, 128, 2, 2, 1>(a, rest, {128, 4 * std::min(d.tiles, kLeft), 1}, s);
         }
     case 128:
         // two workgroups to a CU where there are as many, else twice the steps to a
         // barrier and twice the waves (2048 x 2048, A | A A | B X, us: 25 | 25 | 31 for
         // 27 | 28 | 33 with four waves, and 28 | 29 | 34 with half the steps)
-        if (d.tiles > CBW_NUM_CUS) return launch_tiles<STAGE, PAIR, 128, 2, 2, 1>(a, st, d, s);
-        return launch_tiles<STAGE, PAIR, 128, 2, 4, 2>(a, st, d, s);
+        if (d.tiles > CBW_NUM_CUS) return launch_tiles<STAGE, 128, 2, 2, 1>(a, st, d, s);
+        return launch_tiles<STAGE, 128, 2, 4, 2>(a, st, d, s);
     default:
-        if (d.tiles * d.split > 2 * CBW_NUM_CUS) return launch_tiles<STAGE, PAIR, 64, 2, 2, 1>(a, st, d, s);
-        return launch_tiles<STAGE, PAIR, 64, 2, 2, 2>(a, st, d, s);
+        if (d.tiles * d.split > 2 * CBW_NUM_CUS) return launch_tiles<STAGE, 64, 2, 2, 1>(a, st, d, s);
+        return launch_tiles<STAGE, 64, 2, 2, 2>(a, st, d, s);
     }
-}
-
-template <bool PAIR>
-hipError_t launch_step(const OrthoArgs& a, const StepArgs& st, const OrthoPlan& p, hipStream_t s)
-{
-    const OrthoDeal* d = p.deal[PAIR];
-    hipError_t e = launch_product<GRAM, PAIR>(a, st, d[GRAM], s);
-    if (e == hipSuccess) e = launch_product<SQUARE, PAIR>(a, st, d[SQUARE], s);
-    if (e == hipSuccess) e = launch_product<UPDATE, PAIR>(a, st, d[UPDATE], s);
-    return e;
 }
 
 int64_t round_up(int64_t v, int64_t by) { return (v + by - 1) / by * by; }
@@ -865,14 +835,14 @@ int64_t round_up(int64_t v, int64_t by) { return (v + by - 1) / by * by; }
 // 2000 198 for 164, 6 x 300 x 700 199 for 173, 3 x 333 x 1001 175 for 166; with
 // 4.5, 256 x 2304 166 for 128; with 9.5 as with 7.5.)
 template <typename F>
-OrthoDeal deal(F tiles, int64_t len, bool pair, bool by128, bool by256)
+OrthoDeal deal(F tiles, int64_t len, bool by128, bool by256)
 {
     OrthoDeal d{};
     // (those of 128 are finished whole: both sides are filled up to that)
     d.side = by256 && tiles(256) > kLeft ? 256 : by128 && tiles(128) >= 128 ? 128 : 64;
     d.tiles = (int)tiles(d.side);
     d.split = 1;
-    const int64_t steps = len / (pair ? 32 : 64);
+    const int64_t steps = len / kStep;
     double best = 4.4 + 0.5 * (double)steps - 1.0;   // (no split for less than 1 us)
     for (int s = 2; d.side == 64 && s <= steps && s <= 24 && (int64_t)d.tiles * s <= 2 * CBW_NUM_CUS; ++s) {
         const double us = 7.5 + 0.25 * s + 0.5 * (double)((steps + s - 1) / s);
@@ -893,22 +863,17 @@ OrthoPlan ortho_plan(const cbw_ortho_desc* d)
     if (ortho_narrow_plan(d, &p)) return p;
     p.np = (int)round_up(n, n > 256 ? 128 : 64);
     p.mp = (int)round_up(m, n > 256 ? 128 : 64);
-    // steps on high parts: see above (n itself, not what it is filled up to)
-    if (d->out_dtype == CBW_BF16 && d->a >= 1.f)   // (below 1 small values never grow, and never get their last steps)
-        for (double g = 1.0; p.coarse + 2 < d->steps && g <= 0.14 * (double)n; g *= (double)d->a * d->a) ++p.coarse;
     p.parts = (int)std::min<int64_t>(512, std::max<int64_t>(1, (int64_t)d->rows * d->cols / 8192));
     size_t sums = 0;
-    for (int pair = 0; pair < 2; ++pair) {
-        for (int k = 0; k < 3; ++k) {
-            auto tiles = [&](int side) {
-                const int64_t rows = (p.np + side - 1) / side, cols = (p.mp + side - 1) / side;
-                return d->batch * (k == UPDATE ? rows * cols : rows * (rows + 1) / 2);
-            };
-            OrthoDeal& e = p.deal[pair][k];
-            const bool by128 = p.np % 128 == 0 && p.mp % 128 == 0;
-            e = deal(tiles, k == GRAM ? p.mp : p.np, pair, by128, by128 && k != UPDATE);
-            if (e.split > 1) sums = std::max(sums, (size_t)e.tiles * e.split * e.side * e.side * 4);
-        }
+    for (int k = 0; k < 3; ++k) {
+        auto tiles = [&](int side) {
+            const int64_t rows = (p.np + side - 1) / side, cols = (p.mp + side - 1) / side;
+            return d->batch * (k == UPDATE ? rows * cols : rows * (rows + 1) / 2);
+        };
+        OrthoDeal& e = p.deal[k];
+        const bool by128 = p.np % 128 == 0 && p.mp % 128 == 0;
+        e = deal(tiles, k == GRAM ? p.mp : p.np, by128, by128 && k != UPDATE);
+        if (e.split > 1) sums = std::max(sums, (size_t)e.tiles * e.split * e.side * e.side * 4);
     }
     size_t at = 0;
     auto take = [&](size_t bytes) { return ortho_region(at, bytes); };
@@ -928,19 +893,18 @@ OrthoPlan ortho_plan(const cbw_ortho_desc* d)
 hipError_t launch_orthogonalize(const OrthoArgs& a, const OrthoPlan& p, int steps, hipStream_t s)
 {
     if (p.rows) return launch_ortho_narrow(a, p, steps, s);
-    auto pair = [&](int k) { return k >= p.coarse; };
     ortho_norm_kernel<<<a.batch * a.parts, 256, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    ortho_start_kernel<<<a.batch * (a.np / 64) * (a.mp / 64), 256, 0, s>>>(a, pair(0));
+    ortho_start_kernel<<<a.batch * (a.np / 64) * (a.mp / 64), 256, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     for (int k = 0; k < steps && e == hipSuccess; ++k) {
         StepArgs st{};
         st.from = k & 1;
         st.last = k + 1 == steps;
-        st.pair = pair(k);
-        st.next_pair = pair(k + 1);
-        e = st.pair ? launch_step<true>(a, st, p, s) : launch_step<false>(a, st, p, s);
+        e = launch_product<GRAM>(a, st, p.deal[GRAM], s);
+        if (e == hipSuccess) e = launch_product<SQUARE>(a, st, p.deal[SQUARE], s);
+        if (e == hipSuccess) e = launch_product<UPDATE>(a, st, p.deal[UPDATE], s);
     }
     return e;
 }
