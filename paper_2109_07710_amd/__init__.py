@@ -13,6 +13,7 @@ weight gradient skipping all-zero blocks of the incoming gradient (input
 sparsity), and the dense data gradient.
 """
 import ctypes
+import math
 import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -696,15 +697,17 @@ def ortho_workspace(desc, device="cuda"):
 
 def _matrices(t, d, stride, dtype):
     """Device pointer of the matrices [batch][rows][cols], rows `stride`
-    elements apart throughout; one matrix may be without the first axis, and
-    further axes may be taken together as its columns ([K][R][S][C])."""
+    elements apart throughout; one matrix may be without the first axis.  Adjacent
+    ones may have further axes: the last ones are taken together as a matrix's
+    columns ([K][R][S][C]), those before as the matrices' rows ([E][2K][C])."""
     if not t.is_cuda:
         raise ValueError("expected a device tensor")
     if t.dtype is not dtype:
         raise ValueError("expected a %s tensor, got %s" % (dtype, t.dtype))
     whole = d.batch * d.rows * d.cols
     if stride == d.cols:
-        if t.numel() != whole or not t.is_contiguous():
+        columns = any(math.prod(t.shape[k:]) == d.cols for k in range(t.dim() + 1))
+        if t.numel() != whole or (whole and not columns) or not t.is_contiguous():
             raise ValueError("expected a contiguous tensor of %d matrices of %d x %d, got shape %s, strides %s" % (
                 d.batch, d.rows, d.cols, tuple(t.shape), t.stride()))
     elif whole:
