@@ -18,13 +18,13 @@ def _take(d, *shape, stride=None):
     (256, 2304, 1, (256, 2304)), (256, 2304, 1, (1, 256, 2304)), (32, 72, 1, (32, 3, 3, 8)), (32, 72, 2, (2, 32, 3, 3, 8)), (32, 72, 2, (64, 72)),
     (24, 16, 6, (3, 48, 16)),                       # [E][2K][C], a matrix for each of an expert's two filters
     (24, 16, 6, (3, 2, 24, 16)), (1, 40, 1, (40,)), (40, 1, 1, (40,)), (40, 1, 3, (3, 40)), (5, 7, 0, (0, 5, 7)), (5, 7, 0, (0,)), (6, 6, 2, (2, 6, 6)),
-    (40, 1, 1, (1, 40)), (1, 40, 1, (40, 1))])      # (a vector is the same matrix either way)
+    (8, 24, 3, (24, 24, 1)), (40, 1, 1, (1, 40)), (1, 40, 1, (40, 1))])      # (a vector is the same matrix either way)
 def test_shapes_that_are_the_matrices(rows, cols, batch, shape):
     _take(cb.OrthoDesc.make(rows, cols, batch), *shape)
 
 
 @pytest.mark.parametrize("rows,cols,batch,shape", [
-    (256, 2304, 1, (2304, 256)), (256, 2304, 1, (3, 3, 256, 256)), (8, 24, 3, (3, 24, 8)), (8, 24, 3, (24, 24, 1)), (8, 24, 3, (3 * 8 * 24,)),
+    (256, 2304, 1, (2304, 256)), (256, 2304, 1, (3, 3, 256, 256)), (8, 24, 3, (3, 24, 8)), (8, 24, 3, (3 * 8 * 24,)),
     (8, 24, 3, (2, 8, 24)), (32, 72, 1, (8, 3, 3, 32))])
 def test_shapes_that_are_not(rows, cols, batch, shape):
     with pytest.raises(ValueError, match="expected"):
