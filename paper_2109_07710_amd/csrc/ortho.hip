@@ -14,10 +14,11 @@
 // half-precision rate, which is a fifth of the float32 instructions' time.
 // Every step takes both parts, whatever the type of the result.  High parts alone
 // in the first steps would do for matrices whose singular values are alike, and
-// for those only: with four live rows of 1024, three of five such steps leave an
-// error of 5e-3 to 9e-3 of the 2-norm, where rounding the result to bf16 leaves
-// 1.7e-3, and one live row loses as much in its first step alone, so that no
-// number of such steps follows from the sizes.
+// for those only.  In an emulation of these roundings, four live rows of 1024 and
+// three of five such steps leave an error of 5e-3 to 1e-2 of the 2-norm, where
+// rounding the result to bf16 leaves 1.7e-3; one live row loses 1.5e-3 in its
+// first step, so that no number of such steps follows from the sizes.  (2048 x
+// 2048 to bf16: 505 us with three such steps, 676 without.)
 #include "common.hpp"
 #include "block_kernels.hpp"
 #include "expert_tiles.hpp"
@@ -816,8 +817,9 @@ hipError_t launch_product(const OrthoArgs& a, const StepArgs& st, const OrthoDea
         }
     case 128:
         // two workgroups to a CU where there are as many, else twice the steps to a
-        // barrier and twice the waves (2048 x 2048, A | A A | B X, us: 25 | 25 | 31 for
-        // 27 | 28 | 33 with four waves, and 28 | 29 | 34 with half the steps)
+        // barrier and twice the waves (2048 x 2048, A | A A | B X, us: 40 | 41 | 50 for
+        // 52 | 53 | 60 with four waves and half the steps, and 44 | 45 | 52 with half
+        // the steps)
         if (d.tiles > CBW_NUM_CUS) return launch_tiles<STAGE, 128, 2, 2, 1>(a, st, d, s);
         return launch_tiles<STAGE, 128, 2, 4, 2>(a, st, d, s);
     default:

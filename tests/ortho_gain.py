@@ -19,8 +19,8 @@ A step's own errors are those of ortho_ref, every product on pairs.  Rows and
 columns of zeros stay zeros exactly, since every term of their sums is zero, and
 are left out.  Of second order, b X X^T X and c (X X^T)^2 X leave at most 3 |b| s +
 10 |c| s^3, below 56 |error| of the first a step for s up to 1.22 and the
-coefficients here: less than a ninth while errors are below 2^-9, a factor of
-1.7 over five steps; the bound is taken twice."""
+coefficients here: less than a ninth while an error's singular values are below
+2^-9, a factor of 1.7 over five steps; the bound is taken twice."""
 import torch
 
 from ortho_ref import U32, _product
